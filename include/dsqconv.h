@@ -368,6 +368,134 @@ dsq_status dsq_soft_quantize_bwd(const float *x, const float *grad_y, size_t n,
 dsq_status dsq_conv2d_plan(const dsq_conv_desc *d, int chained, float l_a,
                            char *text, size_t text_bytes);
 
+/* ==== layers of language models ============================================
+ * A linear layer with 4-bit weights that have a scale and a zero point per GROUP of
+ * input channels (32, 64 or 128), for rows of floats and for rows quantized to 8 bits
+ * with a scale each, and the RMS norm that makes such rows.  A row is a token.
+ *
+ *   Rows of floats are float32, float16 or bfloat16 (dsq_dtype); their elements lie side by
+ *   side, and inputs may have any distance from row to row (a `_stride` in elements, 0 for a
+ *   row that repeats).  Zero rows are no error: such a call does nothing.
+ *   At most 2^21 rows, rows of at most 2^20 elements, 2^24 output channels, 2^36 weights;
+ *   DSQ_ERR_UNSUPPORTED beyond, as for an unknown type or group size.
+ *   An input that holds an infinity or a NaN makes its own row NaN or infinite and no other.
+ *
+ * Rows of 8-bit codes: int8 [rows][dsq_code_row_bytes(dim)], codes -127..127, the row's
+ *   length rounded up to a multiple of 128 with code 0 behind the last; the value a code
+ *   stands for is its row's scale times the code.
+ * 4-bit weights: blocks of 16 output channels x 128 input channels, [Np/16][Kp/128][64
+ *   lanes][4 words], Np and Kp rounded up to 128.  Word t of lane 16q + r holds input
+ *   channels 32t + 8q + 0..7 of the block for its output channel r, as byte j = c[j] |
+ *   c[j+4] << 4.  Scales: [Np/16][Kp/group][16] words, each a float32 whose low four bits
+ *   are the zero point (the scale is the number with those bits clear: a float16 or
+ *   bfloat16 scale is kept as it is).  The level of a code is scale * (code - zero).
+ */
+typedef enum { DSQ_F32 = 0, DSQ_F16 = 1, DSQ_BF16 = 2 } dsq_dtype;
+
+/* Sizes (0 on invalid arguments): bytes of a row of 8-bit codes; of the workspace of
+ * dsq_rms_norm_bwd; of packed weights of N output and K input channels; of their scales. */
+size_t dsq_code_row_bytes(int dim);
+size_t dsq_rms_norm_bwd_bytes(int rows, int dim);
+size_t dsq_w4_packed_bytes(int N, int K);
+size_t dsq_w4_scale_bytes(int N, int K, int group);
+
+/* ---- dsq_rms_norm: residual addition, RMS norm, quantization of the rows ----
+ *     h     = x + residual                       (binary32, rounded to dtype)
+ *     r     = 1 / sqrt(mean of h^2 + eps)        (binary64)
+ *     y     = h * r * weight                     (rounded once, to binary32, then dtype)
+ *     amax  = max over the row of |h * weight|
+ *     code  = 127 * h * weight / amax, rounded to the nearest integer, halves to even
+ *             (decided from h and weight exactly: r is no part of it)
+ *     scale = r * amax / 127
+ * A row of zeros has codes 0 and scale 0; a row with an infinity or a NaN (in h or weight)
+ * has codes 0 and scale NaN.
+ *
+ * x          device, [rows] rows of dim elements
+ * residual   device, the same, or NULL: h = x
+ * weight     device, [dim] of dtype, or NULL for ones
+ * eps        finite and > 0 (DSQ_ERR_RANGE)
+ * sum        device, out, [rows][dim] of dtype: h; or NULL
+ * y          device, out, [rows][dim] of dtype; or NULL
+ * codes, scales   device, out, 8-bit rows and float32 [rows]; both or neither
+ *            (codes_bytes is the caller's buffer size)
+ * rstd       device, out, float32 [rows]: r, for the backward pass; or NULL
+ * At least one output is wanted (DSQ_ERR_NULL).  sum or y may be the memory of x or of
+ * residual if that has its rows side by side (stride dim; DSQ_ERR_UNSUPPORTED otherwise);
+ * other overlaps of outputs with inputs or each other are not allowed.
+ */
+dsq_status dsq_rms_norm(const void *x, int64_t x_stride, const void *residual,
+                        int64_t residual_stride, const void *weight,
+                        dsq_dtype dtype, int rows, int dim, float eps, void *sum,
+                        void *y, int8_t *codes, size_t codes_bytes, float *scales,
+                        float *rstd, void *hip_stream);
+
+/* ---- dsq_rms_norm_bwd ------------------------------------------------------
+ * From gradients of y and of the sum to those of x (the residual's is the same) and of
+ * the weight, n = h * r:
+ *     grad_x      = r * (grad_y * weight - n * mean of (grad_y * weight * n)) + grad_sum
+ *     grad_weight = sum over the rows of grad_y * n
+ * For 8-bit rows, grad_y is the gradient of the values that the codes stand for (their
+ * rounding passes gradients straight through).  The result of a call is the same every
+ * time: no atomics.
+ *
+ * h          device: the sum that dsq_rms_norm wrote (x where there was no residual)
+ * rstd       device: what dsq_rms_norm wrote
+ * grad_sum   device, or NULL: no gradient arrives at the sum
+ * grad_x     device, out, [rows][dim] of dtype; may be the memory of h, grad_y or grad_sum
+ *            under the conditions of dsq_rms_norm
+ * grad_weight device, out, float32 [dim], or NULL; overwritten (zeros for zero rows)
+ * workspace  device, dsq_rms_norm_bwd_bytes(rows, dim) bytes, needed for grad_weight alone;
+ *            of no other call that may run at the same time, captured graphs included
+ */
+dsq_status dsq_rms_norm_bwd(const void *h, int64_t h_stride, const void *weight,
+                            const float *rstd, const void *grad_y,
+                            int64_t grad_y_stride, const void *grad_sum,
+                            int64_t grad_sum_stride, dsq_dtype dtype, int rows,
+                            int dim, void *grad_x, float *grad_weight,
+                            void *workspace, size_t workspace_bytes,
+                            void *hip_stream);
+
+/* ---- dsq_pack_weights_w4: once per layer ------------------------------------
+ * w          device, float32 [N][K]; NULL if codes is given
+ * codes      device, uint8 [N][K] (above 15: stored as 15), or NULL
+ * scale, zero   device, float32 and uint8 (above 15: 15) [N][ceil(K / group)]; both or, with
+ *            w, neither.  A scale is kept to 20 significant bits.
+ * With w alone each group gets, in binary32, the range from min(w, 0) to max(w, 0):
+ *     scale = (max - min) / 15, kept to 20 bits;  zero = rint(-min / scale)
+ * and with w in any case  code = clamp(rint(w / scale) + zero, 0, 15); a scale of 0 has
+ * code = zero.
+ */
+dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
+                               const float *scale, const uint8_t *zero, int N, int K,
+                               int group, void *w_packed, size_t w_bytes,
+                               void *w_scales, size_t scale_bytes, void *hip_stream);
+
+/* ---- dsq_linear_w4: float rows ------------------------------------------------
+ *     out[m][n] = bias[n] + sum over groups g of
+ *                 scale[n][g] * sum over k in g of (code[n][k] - zero[n][g]) * x[m][k]
+ * Codes and activations enter the matrix instruction exactly (a float32 activation in three
+ * parts), sums are binary32, and the result is rounded to dtype once.  The zero point's
+ * share is formed from the group's sum of x, so sums reach 15 times that of |x|.
+ * x          device, [M] rows of K elements of dtype
+ * bias       device, [N] of dtype, or NULL
+ * out        device, out, [M] rows of N elements of dtype, out_stride >= N elements from row
+ *            to row; what lies between them is left as it is
+ */
+dsq_status dsq_linear_w4(const void *x, int64_t x_stride, dsq_dtype dtype, int M,
+                         int N, int K, int group, const void *w_packed,
+                         const void *w_scales, const void *bias, void *out,
+                         int64_t out_stride, void *hip_stream);
+
+/* ---- dsq_linear_w4a8: rows of 8-bit codes ---------------------------------------
+ * The same with x[m][k] = code_scales[m] * codes[m][k]: the sums of a group are exact
+ * integers.  dtype is that of bias and out; codes as dsq_rms_norm writes them.
+ */
+dsq_status dsq_linear_w4a8(const int8_t *codes, size_t codes_bytes,
+                           const float *code_scales, int M, int N, int K, int group,
+                           const void *w_packed, const void *w_scales,
+                           const void *bias, dsq_dtype dtype, void *out,
+                           int64_t out_stride, void *hip_stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *dsq_status_string(dsq_status s);
 

@@ -26,6 +26,7 @@ DSQ_CONV_ACT_DENSE3 = 0x20
 DSQ_CONV_NEXT_DENSE3 = 0x40
 DSQ_CONV_NEXT_SUMS_ZERO = 0x80
 DSQ_PACK_CONTAINER, DSQ_PACK_DENSE3 = 0, 1
+DSQ_F32, DSQ_F16, DSQ_BF16 = 0, 1, 2
 
 
 def DSQ_CONV_KERNEL(k):
@@ -36,6 +37,8 @@ EXPORTS = [
     "dsq_quantize_act", "dsq_quantize_act_ex", "dsq_pack_weights", "dsq_pack_weights_for", "dsq_conv2d", "dsq_conv2d_requant", "dsq_conv2d_wq",
     "dsq_soft_quantize_fwd", "dsq_soft_quantize_bwd",
     "dsq_conv2d_plan", "dsq_status_string",
+    "dsq_code_row_bytes", "dsq_rms_norm_bwd_bytes", "dsq_w4_packed_bytes", "dsq_w4_scale_bytes",
+    "dsq_rms_norm", "dsq_rms_norm_bwd", "dsq_pack_weights_w4", "dsq_linear_w4", "dsq_linear_w4a8",
 ]
 
 
@@ -94,6 +97,21 @@ def load_library():
     lib.dsq_soft_quantize_bwd.argtypes = [vp, vp, sz, f, f, f, i, vp, vp, vp]
     lib.dsq_conv2d_plan.restype = i
     lib.dsq_conv2d_plan.argtypes = [C.POINTER(dsq_conv_desc), i, f, C.c_char_p, sz]
+    i64 = C.c_int64
+    for name, args in (("dsq_code_row_bytes", [i]), ("dsq_rms_norm_bwd_bytes", [i, i]), ("dsq_w4_packed_bytes", [i, i]),
+                       ("dsq_w4_scale_bytes", [i, i, i])):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = args
+    lib.dsq_rms_norm.restype = i
+    lib.dsq_rms_norm.argtypes = [vp, i64, vp, i64, vp, i, i, i, f, vp, vp, vp, sz, vp, vp, vp]
+    lib.dsq_rms_norm_bwd.restype = i
+    lib.dsq_rms_norm_bwd.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, i, i, i, vp, vp, vp, sz, vp]
+    lib.dsq_pack_weights_w4.restype = i
+    lib.dsq_pack_weights_w4.argtypes = [vp, vp, vp, vp, i, i, i, vp, sz, vp, sz, vp]
+    lib.dsq_linear_w4.restype = i
+    lib.dsq_linear_w4.argtypes = [vp, i64, i, i, i, i, i, vp, vp, vp, vp, i64, vp]
+    lib.dsq_linear_w4a8.restype = i
+    lib.dsq_linear_w4a8.argtypes = [vp, sz, vp, i, i, i, i, vp, vp, vp, i, vp, i64, vp]
     lib.dsq_status_string.restype = C.c_char_p
     lib.dsq_status_string.argtypes = [i]
     _lib = lib
@@ -284,6 +302,153 @@ def dsq_conv2d_plan(desc, chained=False, l_a=0.0):
     buf = C.create_string_buffer(512)
     _check(load_library().dsq_conv2d_plan(C.byref(desc), int(bool(chained)), l_a, buf, len(buf)))
     return buf.value.decode()
+
+
+# ---------------------------------------------------------------------------
+# Layers of language models.  Rows of floats are tensors of two dimensions whose rows may lie
+# apart (stride(1) is 1); their shapes and type are taken from them.
+# ---------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: DSQ_F32, torch.float16: DSQ_F16, torch.bfloat16: DSQ_BF16}
+
+
+def dsq_code_row_bytes(dim):
+    return int(load_library().dsq_code_row_bytes(dim))
+
+
+def dsq_rms_norm_bwd_bytes(rows, dim):
+    return int(load_library().dsq_rms_norm_bwd_bytes(rows, dim))
+
+
+def dsq_w4_packed_bytes(N, K):
+    return int(load_library().dsq_w4_packed_bytes(N, K))
+
+
+def dsq_w4_scale_bytes(N, K, group):
+    return int(load_library().dsq_w4_scale_bytes(N, K, group))
+
+
+def _here(t, name):
+    """A device tensor of the current device: the stream and the kernel are that device's."""
+    if not isinstance(t, torch.Tensor):
+        raise DsqError(1, "%s is a required tensor" % name) if t is None else TypeError("%s: expected a tensor" % name)
+    if not t.is_cuda:
+        raise TypeError("libdsqconv takes device tensors")
+    if t.get_device() != torch.cuda.current_device():
+        raise TypeError("%s is on another device than the current one" % name)
+    return t
+
+
+def _rows(t, name, shape=None, dtype=None, strided=True, allow_none=False):
+    """(address, distance of rows) of a tensor [rows, elements], (None, 0) where it may be None."""
+    if t is None and allow_none:
+        return None, 0
+    _here(t, name)
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise DsqError(4, "%s has the shape %s%s" % (name, list(t.shape), "" if shape is None else ", expected %s" % list(shape)))
+    if dtype is None:
+        if t.dtype not in _DTYPES:
+            raise TypeError("%s: expected float32, float16 or bfloat16, got %s" % (name, t.dtype))
+    elif t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.numel() and t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError("%s: the elements of a row must lie side by side" % name)
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if not strided and stride != t.shape[1]:
+        raise TypeError("%s must be contiguous" % name)
+    return t.data_ptr(), stride
+
+
+def _vector(t, name, n, dtype, allow_none=False):
+    """Address of a contiguous tensor of n elements."""
+    if t is None and allow_none:
+        return None
+    if _here(t, name).dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    if t.numel() != n:
+        raise DsqError(4, "%s has %d elements, expected %d" % (name, t.numel(), n))
+    return t.data_ptr()
+
+
+def _bytes(t, name, allow_none=False):
+    """(address, size) of a uint8 buffer."""
+    if t is None and allow_none:
+        return None, 0
+    if _here(t, name).dtype != torch.uint8:
+        raise TypeError("%s: expected %s, got %s" % (name, torch.uint8, t.dtype))
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    return t.data_ptr(), t.numel()
+
+
+def _code_rows(t, name, rows, dim):
+    """Address of int8 rows with their pitch."""
+    return _rows(t, name, (rows, dsq_code_row_bytes(dim)), torch.int8, strided=False)[0]
+
+
+def dsq_rms_norm(x, residual, weight, eps, sum_out, y, codes, scales, rstd, stream=None):
+    """x, residual [rows, dim]; sum_out, y [rows, dim]; codes int8 [rows, dsq_code_row_bytes(dim)]; all but x may be None."""
+    xp, xs = _rows(x, "x")
+    (rows, dim), dt = x.shape, x.dtype
+    rp, rs = _rows(residual, "residual", x.shape, dt, allow_none=True)
+    _check(load_library().dsq_rms_norm(
+        xp, xs, rp, rs, _vector(weight, "weight", dim, dt, True), _DTYPES[dt], rows, dim, eps,
+        _rows(sum_out, "sum_out", x.shape, dt, False, True)[0], _rows(y, "y", x.shape, dt, False, True)[0],
+        None if codes is None else _code_rows(codes, "codes", rows, dim), 0 if codes is None else codes.numel(),
+        _vector(scales, "scales", rows, torch.float32, True), _vector(rstd, "rstd", rows, torch.float32, True), _stream(stream)))
+
+
+def dsq_rms_norm_bwd(h, weight, rstd, grad_y, grad_sum, grad_x, grad_weight, workspace, stream=None):
+    """h, grad_y, grad_sum, grad_x [rows, dim]; grad_weight float32 [dim]; workspace uint8 of dsq_rms_norm_bwd_bytes(rows, dim)."""
+    hp, hs = _rows(h, "h")
+    (rows, dim), dt = h.shape, h.dtype
+    gp, gs = _rows(grad_y, "grad_y", h.shape, dt)
+    sp, ss = _rows(grad_sum, "grad_sum", h.shape, dt, allow_none=True)
+    ws, nbytes = _bytes(workspace, "workspace", True)
+    _check(load_library().dsq_rms_norm_bwd(
+        hp, hs, _vector(weight, "weight", dim, dt, True), _vector(rstd, "rstd", rows, torch.float32), gp, gs, sp, ss,
+        _DTYPES[dt], rows, dim, _rows(grad_x, "grad_x", h.shape, dt, False)[0],
+        _vector(grad_weight, "grad_weight", dim, torch.float32, True), ws, nbytes, _stream(stream)))
+
+
+def dsq_pack_weights_w4(w, codes, scale, zero, N, K, group, w_packed, w_scales, stream=None):
+    """w float32 or codes uint8 [N, K]; scale float32 and zero uint8 [N, ceil(K / group)] or None."""
+    groups = N * -(-K // group) if group > 0 else 0
+    wp, wn = _bytes(w_packed, "w_packed")
+    sp, sn = _bytes(w_scales, "w_scales")
+    _check(load_library().dsq_pack_weights_w4(
+        _vector(w, "w", N * K, torch.float32, True), _vector(codes, "codes", N * K, torch.uint8, True),
+        _vector(scale, "scale", groups, torch.float32, True), _vector(zero, "zero", groups, torch.uint8, True),
+        N, K, group, wp, wn, sp, sn, _stream(stream)))
+
+
+def _packed(w_packed, w_scales, N, K, group):
+    wp, wn = _bytes(w_packed, "w_packed")
+    sp, sn = _bytes(w_scales, "w_scales")
+    if wn < dsq_w4_packed_bytes(N, K) or sn < dsq_w4_scale_bytes(N, K, group):
+        raise DsqError(7, "w_packed or w_scales is smaller than a layer of %d x %d in groups of %d" % (N, K, group))
+    return wp, sp
+
+
+def dsq_linear_w4(x, w_packed, w_scales, N, K, group, bias, out, stream=None):
+    """x [M, K], out [M, N], bias [N] or None, of one type."""
+    xp, xs = _rows(x, "x", (x.shape[0], K) if isinstance(x, torch.Tensor) and x.dim() == 2 else None)
+    op, os_ = _rows(out, "out", (x.shape[0], N), x.dtype)
+    wp, sp = _packed(w_packed, w_scales, N, K, group)
+    _check(load_library().dsq_linear_w4(xp, xs, _DTYPES[x.dtype], x.shape[0], N, K, group, wp, sp,
+                                        _vector(bias, "bias", N, x.dtype, True), op, os_, _stream(stream)))
+
+
+def dsq_linear_w4a8(codes, scales, w_packed, w_scales, N, K, group, bias, out, stream=None):
+    """codes int8 [M, dsq_code_row_bytes(K)], scales float32 [M]; out [M, N] and bias [N] or None, of one type."""
+    op, os_ = _rows(out, "out", (out.shape[0], N) if isinstance(out, torch.Tensor) and out.dim() == 2 else None)
+    M = out.shape[0]
+    cp = _code_rows(codes, "codes", M, K)
+    wp, sp = _packed(w_packed, w_scales, N, K, group)
+    _check(load_library().dsq_linear_w4a8(cp, codes.numel(), _vector(scales, "scales", M, torch.float32), M, N, K, group, wp, sp,
+                                          _vector(bias, "bias", N, out.dtype, True), _DTYPES[out.dtype], op, os_, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
