@@ -129,6 +129,7 @@ class _NoMarshal:
         return None
 
     conv2d = conv2d_requant = conv2d_wq = soft_quantize_fwd = soft_quantize_bwd = quantize_act
+    rms_norm = rms_norm_bwd = linear_w4 = linear_w4a8 = quantize_act
 
 
 def load_marshal():
@@ -148,6 +149,9 @@ def load_marshal():
         module.init(dsq_conv_desc, *(C.cast(getattr(lib, name), C.c_void_p).value for name in
                                      ("dsq_quantize_act", "dsq_conv2d", "dsq_conv2d_requant", "dsq_conv2d_wq",
                                       "dsq_soft_quantize_fwd", "dsq_soft_quantize_bwd")))
+        module.init_lm(*(C.cast(getattr(lib, name), C.c_void_p).value for name in
+                         ("dsq_rms_norm", "dsq_rms_norm_bwd", "dsq_linear_w4", "dsq_linear_w4a8", "dsq_code_row_bytes",
+                          "dsq_w4_packed_bytes", "dsq_w4_scale_bytes")))
         _marshal = module
     return _marshal
 
@@ -390,6 +394,11 @@ def _code_rows(t, name, rows, dim):
 
 def dsq_rms_norm(x, residual, weight, eps, sum_out, y, codes, scales, rstd, stream=None):
     """x, residual [rows, dim]; sum_out, y [rows, dim]; codes int8 [rows, dsq_code_row_bytes(dim)]; all but x may be None."""
+    status = (_marshal or load_marshal()).rms_norm(x, residual, weight, eps, sum_out, y, codes, scales, rstd, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
     xp, xs = _rows(x, "x")
     (rows, dim), dt = x.shape, x.dtype
     rp, rs = _rows(residual, "residual", x.shape, dt, allow_none=True)
@@ -402,6 +411,11 @@ def dsq_rms_norm(x, residual, weight, eps, sum_out, y, codes, scales, rstd, stre
 
 def dsq_rms_norm_bwd(h, weight, rstd, grad_y, grad_sum, grad_x, grad_weight, workspace, stream=None):
     """h, grad_y, grad_sum, grad_x [rows, dim]; grad_weight float32 [dim]; workspace uint8 of dsq_rms_norm_bwd_bytes(rows, dim)."""
+    status = (_marshal or load_marshal()).rms_norm_bwd(h, weight, rstd, grad_y, grad_sum, grad_x, grad_weight, workspace, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
     hp, hs = _rows(h, "h")
     (rows, dim), dt = h.shape, h.dtype
     gp, gs = _rows(grad_y, "grad_y", h.shape, dt)
@@ -434,6 +448,11 @@ def _packed(w_packed, w_scales, N, K, group):
 
 def dsq_linear_w4(x, w_packed, w_scales, N, K, group, bias, out, stream=None):
     """x [M, K], out [M, N], bias [N] or None, of one type."""
+    status = (_marshal or load_marshal()).linear_w4(x, w_packed, w_scales, N, K, group, bias, out, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
     xp, xs = _rows(x, "x", (x.shape[0], K) if isinstance(x, torch.Tensor) and x.dim() == 2 else None)
     op, os_ = _rows(out, "out", (x.shape[0], N), x.dtype)
     wp, sp = _packed(w_packed, w_scales, N, K, group)
@@ -443,6 +462,11 @@ def dsq_linear_w4(x, w_packed, w_scales, N, K, group, bias, out, stream=None):
 
 def dsq_linear_w4a8(codes, scales, w_packed, w_scales, N, K, group, bias, out, stream=None):
     """codes int8 [M, dsq_code_row_bytes(K)], scales float32 [M]; out [M, N] and bias [N] or None, of one type."""
+    status = (_marshal or load_marshal()).linear_w4a8(codes, scales, w_packed, w_scales, N, K, group, bias, out, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
     op, os_ = _rows(out, "out", (out.shape[0], N) if isinstance(out, torch.Tensor) and out.dim() == 2 else None)
     M = out.shape[0]
     cp = _code_rows(codes, "codes", M, K)

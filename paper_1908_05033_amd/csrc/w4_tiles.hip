@@ -1,0 +1,299 @@
+// Many rows times group-scaled 4-bit weights (8-bit codes or 16-bit floats): a tiled product on the 32x32 matrix instructions.
+//
+// A workgroup of four waves owns 32 * MT rows x 128 output channels.  Blocks of 128 input channels of its rows go through
+// LDS (rows padded by 16 bytes: reads of a column of 16-byte units are free of bank conflicts); a wave takes 32 channels,
+// whose codes come from global memory in lane order, and all rows, so that a code is unpacked once for 32 * MT rows.  With the rows as
+// the first operand a lane holds one output channel: its scale and zero point are one word a group.
+//
+// 8-bit rows: the operand is code - z as bytes, a group's sum an exact integer, converted and scaled once a group (two
+// vector instructions an element: these, not the matrix instruction, bound the kernel at groups of 128 and below).
+// Floats: the operand is the code, and the group's sum of x, from the staging of the rows, carries the zero point.
+#include "w4_device.h"
+
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v16i __attribute__((ext_vector_type(16)));
+
+template <int XT>
+struct Tile {
+    static constexpr int ES = XT == DSQ_T_I8 ? 1 : 2;
+    static constexpr int ROW = 128 * ES, PITCH = ROW + 16;            // bytes of a block's row in LDS
+    static constexpr int UNITS = ROW / 16;                            // 16-byte units of a row
+};
+
+// Code - zero of a word's eight codes as bytes: 128 + code - zero is between 113 and 143, without carries from byte to byte.
+__device__ __forceinline__ void levels_i8(uint32_t w, uint32_t plus, int &lo, int &hi)
+{
+    lo = (int)(((w & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
+    hi = (int)((((w >> 4) & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
+}
+
+// Results of a wave's tile of 32 rows: row 8 * (c / 4) + 4h + c % 4, the lane's channel n.
+template <int XT, int OT>
+__device__ __forceinline__ void store_tile(const DsqW4Args &a, const v16f &sum, int64_t m0, int n, int h)
+{
+    typedef typename Element<OT>::type E;
+    if (n >= a.N) return;
+    const float bias = a.bias ? (float)((const E *)a.bias)[n] : 0.0f;
+    E *out = (E *)a.out + n;
+    float scale[16];
+    if constexpr (XT == DSQ_T_I8)
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const int64_t m = m0 + 8 * (c / 4) + 4 * h + c % 4;
+            scale[c] = a.x_scale[m < a.M ? m : a.M - 1];
+        }
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        const int64_t m = m0 + 8 * (c / 4) + 4 * h + c % 4;
+        float o = XT == DSQ_T_I8 ? sum[c] * scale[c] : sum[c];
+        if (a.bias) o += bias;
+        if (m < a.M) out[m * a.out_stride] = (E)o;
+    }
+}
+
+// MT: tiles of 32 rows; WN x WK waves: 32 output channels each, and every WK-th block of input channels; GPB: groups of a block.
+template <int XT, int MT, int WN, int WK, int GPB>
+__global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, int tiles_m, int total, int xcd_chunk)
+{
+    typedef Tile<XT> L;
+    constexpr bool INT = XT == DSQ_T_I8;
+    constexpr int SPG = 4 / GPB;                                      // steps of 32 channels in a group
+    constexpr int THREADS = 64 * WN * WK, ROWS = 32 * MT, BLOCK = ROWS * L::PITCH;
+    constexpr int LOADS = ROWS * L::UNITS * WK / THREADS;             // 16-byte units a thread stages
+    constexpr int XSUM = INT ? 0 : GPB * ROWS;                        // sums of x of a block's groups
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][WK] blocks, then [2][WK] sums
+    float *xsums = reinterpret_cast<float *>(lds + 2 * WK * BLOCK);
+
+    // Workgroups are dealt to the 8 XCDs in turn: each gets a contiguous range of tiles, the row tiles of one channel tile
+    // together, so that its weights are read into one L2 only
+    const int logical = ((int)blockIdx.x & 7) * xcd_chunk + ((int)blockIdx.x >> 3);
+    if (logical >= total) return;
+    const int nt = logical / tiles_m;
+    const int64_t m0 = (int64_t)(logical - nt * tiles_m) * ROWS;
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wn = wave % WN, wk = wave / WN;
+    const int KB = dsq_w4_round(a.K) / 128, Gp = KB * GPB, iters = (KB + WK - 1) / WK;
+    const int n0 = nt * 32 * WN + 32 * wn;
+    // this lane's channel: 16-channel block (r / 16), column r % 16; its halves of 16 input channels
+    const size_t ct = (size_t)(n0 / 16 + r / 16);
+    const v4u *w = reinterpret_cast<const v4u *>(a.w) + ct * KB * 64 + 32 * h + r % 16;
+    const uint32_t *sc = a.scales + ct * Gp * 16 + r % 16;
+
+    v16f sum[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 16; ++c) sum[i][c] = 0.0f;
+
+    const int unit = threadIdx.x % L::UNITS, line0 = threadIdx.x / L::UNITS;
+    constexpr int LINES = THREADS / L::UNITS;                         // rows a load instruction of the workgroup covers
+    v4u xr[LOADS];
+    auto load_rows = [&](int it) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int line = line0 + j * LINES, row = line % ROWS, b = it * WK + line / ROWS;
+            int64_t m = m0 + row;
+            m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
+            if constexpr (INT) {
+                // (blocks past the last one meet no weights)
+                xr[j] = *reinterpret_cast<const v4u *>((const char *)a.x + m * a.x_stride + 128 * (b < KB ? b : KB - 1) + 16 * unit);
+            } else {
+                const Frag<XT> f = load_frag<XT>((const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
+                xr[j] = __builtin_bit_cast(v4u, f.v);
+            }
+        }
+    };
+    auto store_rows = [&](int to) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int line = line0 + j * LINES, row = line % ROWS, k = line / ROWS;
+            *reinterpret_cast<v4u *>(lds + (to * WK + k) * BLOCK + row * L::PITCH + 16 * unit) = xr[j];
+            if constexpr (!INT) {
+                // the sum of a group of x: eight channels a lane, 4 * SPG lanes side by side
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t pair = xr[j][i];       // (a bit_cast of the vector's element itself takes element 0)
+                    if constexpr (XT == DSQ_T_BF16) {
+                        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+                        s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, s, false);
+                    } else {
+                        const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+                        s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), ones, s, false);
+                    }
+                }
+#pragma unroll
+                for (int off = 1; off < 4 * SPG; off *= 2) s += __shfl_xor(s, off);
+                if (unit % (4 * SPG) == 0) xsums[(to * WK + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
+            }
+        }
+    };
+    auto load_weights = [&](int it, v4u (&to)[2], uint32_t (&s)[GPB]) {
+        int b = it * WK + wk;
+        b = b < KB ? b : KB - 1;
+        to[0] = w[(size_t)b * 64];
+        to[1] = w[(size_t)b * 64 + 16];
+#pragma unroll
+        for (int g = 0; g < GPB; ++g) s[g] = sc[(size_t)(b * GPB + g) * 16];
+    };
+    // One block of input channels from LDS area `from`.
+    auto block = [&](int from, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) {
+        const char *base = lds + (from * WK + wk) * BLOCK + r * L::PITCH + 16 * L::ES * h;
+        const float *xsum = xsums + (from * WK + wk) * XSUM;
+        // Units of one group and 32 rows: the matrix instructions of a unit stand beside the scaling of the one before.  (Left to
+        // itself the compiler reads the rows of all units first and spills.)
+        v16f facc[2];
+        v16i iacc[2];
+        v4i lev[SPG];
+        auto scaled = [&](int u) {
+            const int g = u / MT, i = u % MT;
+            const float scale = __uint_as_float(sv[g] & ~15u);
+            if constexpr (INT) {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) sum[i][c] = __builtin_fmaf(scale, (float)iacc[u & 1][c], sum[i][c]);
+            } else {
+                const float shift = -scale * (float)(sv[g] & 15u);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const v4f xs = *reinterpret_cast<const v4f *>(xsum + g * ROWS + 32 * i + 8 * c + 4 * h);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        sum[i][4 * c + k] = __builtin_fmaf(shift, xs[k], __builtin_fmaf(scale, facc[u & 1][4 * c + k], sum[i][4 * c + k]));
+                }
+            }
+            // (done here: the compiler would move the scaling of a whole block behind it, and spill the units' sums)
+            asm volatile("" : "+v"(sum[i]));
+        };
+#pragma unroll
+        for (int u = 0; u < GPB * MT; ++u) {
+            const int g = u / MT, i = u % MT;
+            if constexpr (INT) {
+                if (i == 0) {
+                    const uint32_t plus = 0x80808080u - (sv[g] & 15u) * 0x01010101u;
+#pragma unroll
+                    for (int t = 0; t < SPG; ++t) {
+                        int p0, p1, p2, p3;
+                        levels_i8(wv[0][g * SPG + t], plus, p0, p1);
+                        levels_i8(wv[1][g * SPG + t], plus, p2, p3);
+                        lev[t] = (v4i){p0, p1, p2, p3};
+                    }
+                }
+                v16i acc = {};
+#pragma unroll
+                for (int t = 0; t < SPG; ++t) {
+                    const v4i x = *reinterpret_cast<const v4i *>(base + 32 * i * L::PITCH + 32 * (g * SPG + t));
+                    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, lev[t], acc, 0, 0, 0);
+                }
+                iacc[u & 1] = acc;
+            } else {
+                v16f acc = {};
+#pragma unroll
+                for (int t = 0; t < SPG; ++t)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const char *p = base + 32 * i * L::PITCH + 64 * (g * SPG + t) + 16 * k;
+                        if constexpr (XT == DSQ_T_BF16)
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(p), codes_bf16(wv[k][g * SPG + t]), acc, 0, 0, 0);
+                        else
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(p), codes_f16(wv[k][g * SPG + t]), acc, 0, 0, 0);
+                    }
+                facc[u & 1] = acc;
+            }
+            if (u > 0) scaled(u - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        scaled(GPB * MT - 1);
+    };
+
+    // Two sets of weight registers in turn (a copy of the prefetched set would wait for it): while a block is multiplied,
+    // the next one's rows and weights are under way.  What is fetched past the end is not used.
+    v4u wa[2], wb[2];
+    uint32_t sa[GPB], sb[GPB];
+    load_rows(0);
+    load_weights(0, wa, sa);
+    store_rows(0);
+    __syncthreads();
+    for (int it = 0; it < iters; it += 2) {
+        load_rows(it + 1);
+        load_weights(it + 1, wb, sb);
+        __builtin_amdgcn_sched_barrier(0);
+        if (WK == 1 || it * WK + wk < KB) block(0, wa, sa);
+        if (it + 1 >= iters) break;
+        store_rows(1);
+        __syncthreads();
+        load_rows(it + 2);
+        load_weights(it + 2, wa, sa);
+        __builtin_amdgcn_sched_barrier(0);
+        if (WK == 1 || (it + 1) * WK + wk < KB) block(1, wb, sb);
+        if (it + 2 >= iters) break;
+        store_rows(0);
+        __syncthreads();
+    }
+    if constexpr (WK > 1) {
+        // the waves of a channel tile join their sums
+        __syncthreads();
+        v16f *part = reinterpret_cast<v16f *>(lds);                   // [wave][row tile][lane]
+#pragma unroll
+        for (int i = 0; i < MT; ++i) part[(wave * MT + i) * 64 + lane] = sum[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (i % WK != wk) continue;
+            sum[i] = part[(wn * MT + i) * 64 + lane];
+#pragma unroll
+            for (int k = 1; k < WK; ++k) sum[i] += part[((k * WN + wn) * MT + i) * 64 + lane];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        if (WK > 1 && i % WK != wk) continue;
+        const int64_t m = m0 + 32 * i;
+        if (!INT) store_tile<XT, INT ? DSQ_T_F32 : XT>(a, sum[i], m, n0 + r, h);
+        else if (a.out_type == DSQ_T_BF16) store_tile<XT, DSQ_T_BF16>(a, sum[i], m, n0 + r, h);
+        else if (a.out_type == DSQ_T_F16) store_tile<XT, DSQ_T_F16>(a, sum[i], m, n0 + r, h);
+        else store_tile<XT, DSQ_T_F32>(a, sum[i], m, n0 + r, h);
+    }
+}
+
+template <int XT, int MT, int WN, int WK, int GPB>
+hipError_t launch_of(const DsqW4Args &a, hipStream_t stream)
+{
+    typedef Tile<XT> L;
+    constexpr int STAGE = 2 * WK * (32 * MT * L::PITCH + (XT == DSQ_T_I8 ? 0 : GPB * 32 * MT * 4));
+    constexpr int JOIN = WK > 1 ? WN * WK * MT * 64 * 64 : 0, LDS = STAGE > JOIN ? STAGE : JOIN;
+    const int64_t tiles_m = ((int64_t)a.M + 32 * MT - 1) / (32 * MT), tiles_n = ((int64_t)a.N + 32 * WN - 1) / (32 * WN);
+    const int64_t total = tiles_m * tiles_n, xcd_chunk = (total + 7) / 8;
+    if (xcd_chunk * 8 * 64 * WN * WK >= 1LL << 32) return hipErrorInvalidConfiguration;
+    auto kern = w4_tiles_kernel<XT, MT, WN, WK, GPB>;
+    if (LDS > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e != hipSuccess) return e;
+    }
+    kern<<<(unsigned)(8 * xcd_chunk), 64 * WN * WK, LDS, stream>>>(a, (int)tiles_m, (int)total, (int)xcd_chunk);
+    return hipGetLastError();
+}
+
+template <int XT, int MT, int WN, int WK>
+hipError_t launch_groups(const DsqW4Args &a, hipStream_t stream)
+{
+    return a.group == 32 ? launch_of<XT, MT, WN, WK, 4>(a, stream)
+           : a.group == 64 ? launch_of<XT, MT, WN, WK, 2>(a, stream) : launch_of<XT, MT, WN, WK, 1>(a, stream);
+}
+
+template <int XT>
+hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
+{
+    const int64_t large = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
+    if (large >= 256) return launch_groups<XT, 4, 4, 1>(a, stream);
+    return launch_groups<XT, 2, 2, 4>(a, stream);
+}
+
+}  // namespace
+
+hipError_t dsq_launch_w4_tiles(const DsqW4Args &a, hipStream_t stream)
+{
+    return a.x_type == DSQ_T_I8 ? launch_tiles<DSQ_T_I8>(a, stream)
+           : a.x_type == DSQ_T_F16 ? launch_tiles<DSQ_T_F16>(a, stream) : launch_tiles<DSQ_T_BF16>(a, stream);
+}
