@@ -28,7 +28,8 @@ struct Frag<DSQ_T_I8> {
     long v;
 };
 
-template <int XT>
+// (WHOLE: channels k..k+7 exist.  Callers branch on the block and not here: behind a branch at each load it would be waited for.)
+template <int XT, bool WHOLE>
 __device__ __forceinline__ Frag<XT> load_frag(const void *row, int k, int K, bool live)
 {
     Frag<XT> f = {};
@@ -38,14 +39,18 @@ __device__ __forceinline__ Frag<XT> load_frag(const void *row, int k, int K, boo
     } else {
         typedef typename Element<XT>::type E;
         const E *p = (const E *)row + k;
-        if (live && k + 8 <= K) {
-            const Side<E, 8> s = load_side<E, 8>(p);
+        if constexpr (WHOLE) {
+            if (live) {
+                const Side<E, 8> s = load_side<E, 8>(p);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f.v[i] = s.at[i];
+                for (int i = 0; i < 8; ++i) f.v[i] = s.at[i];
+            }
         } else if (live) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < K) f.v[i] = p[i];
+            for (int i = 0; i < 8; ++i) {
+                const E v = ((const E *)row)[k + i < K ? k + i : K - 1];
+                f.v[i] = k + i < K ? v : (E)0.0f;
+            }
         }
     }
     return f;

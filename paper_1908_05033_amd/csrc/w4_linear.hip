@@ -51,8 +51,12 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void w4_rows_kernel(DsqW4Args a)
                 const int64_t m = m0 + 16 * i + r;
                 const void *row = (const char *)a.x + m * a.x_stride * (int64_t)e;
                 Frag<XT> f[4];
+                if (128 * (b + 1) <= a.K)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) f[t] = load_frag<XT>(row, 128 * b + 32 * t + 8 * q, a.K, m < a.M);
+                    for (int t = 0; t < 4; ++t) f[t] = load_frag<XT, true>(row, 128 * b + 32 * t + 8 * q, a.K, m < a.M);
+                else
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) f[t] = load_frag<XT, false>(row, 128 * b + 32 * t + 8 * q, a.K, m < a.M);
 #pragma unroll
                 for (int g = 0; g < GPB; ++g) {
                     Sums<XT> s = {};

@@ -8,6 +8,8 @@
 // 8-bit rows: the operand is code - z as bytes, a group's sum an exact integer, converted and scaled once a group (two
 // vector instructions an element: these, not the matrix instruction, bound the kernel at groups of 128 and below).
 // Floats: the operand is the code, and the group's sum of x, from the staging of the rows, carries the zero point.
+#include <type_traits>
+
 #include "w4_device.h"
 
 namespace {
@@ -27,6 +29,22 @@ __device__ __forceinline__ void levels_i8(uint32_t w, uint32_t plus, int &lo, in
 {
     lo = (int)(((w & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
     hi = (int)((((w >> 4) & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
+}
+
+// The sum over 4, 8 or 16 lanes side by side, in each of them: lanes exchanged by one and by two, then halves and rows of 16 mirrored.
+template <int CONTROL>
+__device__ __forceinline__ float plus_lane(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CONTROL, 0xF, 0xF, true));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v = plus_lane<0xB1>(v);
+    v = plus_lane<0x4E>(v);
+    if (LANES > 4) v = plus_lane<0x141>(v);
+    if (LANES > 8) v = plus_lane<0x140>(v);
+    return v;
 }
 
 // Results of a wave's tile of 32 rows: row 8 * (c / 4) + 4h + c % 4, the lane's channel n.
@@ -89,8 +107,8 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
 
     const int unit = threadIdx.x % L::UNITS, line0 = threadIdx.x / L::UNITS;
     constexpr int LINES = THREADS / L::UNITS;                         // rows a load instruction of the workgroup covers
-    v4u xr[LOADS];
-    auto load_rows = [&](int it) {
+    v4u xa[LOADS], xb[LOADS];
+    auto load_as = [&](int it, v4u (&xr)[LOADS], auto whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, b = it * WK + line / ROWS;
@@ -100,12 +118,16 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 // (blocks past the last one meet no weights)
                 xr[j] = *reinterpret_cast<const v4u *>((const char *)a.x + m * a.x_stride + 128 * (b < KB ? b : KB - 1) + 16 * unit);
             } else {
-                const Frag<XT> f = load_frag<XT>((const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
+                const Frag<XT> f = load_frag<XT, whole.value>((const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
                 xr[j] = __builtin_bit_cast(v4u, f.v);
             }
         }
     };
-    auto store_rows = [&](int to) {
+    auto load_rows = [&](int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
+        if (INT || 128 * WK * (it + 1) <= a.K) load_as(it, xr, std::true_type());
+        else load_as(it, xr, std::false_type());
+    };
+    auto store_rows = [&](int to, const v4u (&xr)[LOADS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, k = line / ROWS;
@@ -124,30 +146,45 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                         s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), ones, s, false);
                     }
                 }
-#pragma unroll
-                for (int off = 1; off < 4 * SPG; off *= 2) s += __shfl_xor(s, off);
+                s = lanes_sum<4 * SPG>(s);
                 if (unit % (4 * SPG) == 0) xsums[(to * WK + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
             }
         }
     };
-    auto load_weights = [&](int it, v4u (&to)[2], uint32_t (&s)[GPB]) {
-        int b = it * WK + wk;
-        b = b < KB ? b : KB - 1;
+    auto load_weights = [&](int it, v4u (&to)[2], uint32_t (&s)[GPB]) __attribute__((always_inline)) {
+        // (past the end: the last block's with scales of 0)
+        const bool live = it * WK + wk < KB;
+        const int b = live ? it * WK + wk : KB - 1;
         to[0] = w[(size_t)b * 64];
         to[1] = w[(size_t)b * 64 + 16];
 #pragma unroll
-        for (int g = 0; g < GPB; ++g) s[g] = sc[(size_t)(b * GPB + g) * 16];
+        for (int g = 0; g < GPB; ++g) {
+            s[g] = sc[(size_t)(b * GPB + g) * 16];
+            if (!live) s[g] = 0;
+        }
     };
     // One block of input channels from LDS area `from`.
-    auto block = [&](int from, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) {
+    auto block = [&](int from, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) __attribute__((always_inline)) {
         const char *base = lds + (from * WK + wk) * BLOCK + r * L::PITCH + 16 * L::ES * h;
         const float *xsum = xsums + (from * WK + wk) * XSUM;
-        // Units of one group and 32 rows: the matrix instructions of a unit stand beside the scaling of the one before.  (Left to
-        // itself the compiler reads the rows of all units first and spills.)
+        // Units of one group and 32 rows: the matrix instructions of a unit stand beside the scaling of the one before, and its
+        // rows are read from LDS one unit ahead.  (Left to itself the compiler reads the rows of all units first and spills, or
+        // reads each operand right before its instruction and waits.)
+        constexpr int XF = INT ? SPG : 2 * SPG;           // operands of a unit's rows
+        constexpr int PART = XF < 4 ? XF : 4, PARTS = XF / PART;      // ... of which so many are read ahead
+        v4i xf[2][PART];
         v16f facc[2];
         v16i iacc[2];
         v4i lev[SPG];
-        auto scaled = [&](int u) {
+        auto read_rows = [&](int p) __attribute__((always_inline)) {
+            const int g = p / PARTS / MT, i = p / PARTS % MT;
+#pragma unroll
+            for (int j = 0; j < PART; ++j) {
+                const int t = p % PARTS * PART + j;
+                xf[p & 1][j] = *reinterpret_cast<const v4i *>(base + 32 * i * L::PITCH + (INT ? 32 * (g * SPG + t) : 64 * (g * SPG + t / 2) + 16 * (t % 2)));
+            }
+        };
+        auto scaled = [&](int u) __attribute__((always_inline)) {
             const int g = u / MT, i = u % MT;
             const float scale = __uint_as_float(sv[g] & ~15u);
             if constexpr (INT) {
@@ -166,9 +203,12 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             // (done here: the compiler would move the scaling of a whole block behind it, and spill the units' sums)
             asm volatile("" : "+v"(sum[i]));
         };
+        read_rows(0);
 #pragma unroll
-        for (int u = 0; u < GPB * MT; ++u) {
-            const int g = u / MT, i = u % MT;
+        for (int p = 0; p < GPB * MT * PARTS; ++p) {
+            const int u = p / PARTS, g = u / MT, i = u % MT;
+            if (p + 1 < GPB * MT * PARTS) read_rows(p + 1);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (INT) {
                 if (i == 0) {
                     const uint32_t plus = 0x80808080u - (sv[g] & 15u) * 0x01010101u;
@@ -182,53 +222,52 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 }
                 v16i acc = {};
 #pragma unroll
-                for (int t = 0; t < SPG; ++t) {
-                    const v4i x = *reinterpret_cast<const v4i *>(base + 32 * i * L::PITCH + 32 * (g * SPG + t));
-                    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, lev[t], acc, 0, 0, 0);
-                }
+                for (int t = 0; t < SPG; ++t) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(xf[p & 1][t], lev[t], acc, 0, 0, 0);
                 iacc[u & 1] = acc;
             } else {
                 v16f acc = {};
+                if (p % PARTS) acc = facc[u & 1];
 #pragma unroll
-                for (int t = 0; t < SPG; ++t)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const char *p = base + 32 * i * L::PITCH + 64 * (g * SPG + t) + 16 * k;
-                        if constexpr (XT == DSQ_T_BF16)
-                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(p), codes_bf16(wv[k][g * SPG + t]), acc, 0, 0, 0);
-                        else
-                            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(p), codes_f16(wv[k][g * SPG + t]), acc, 0, 0, 0);
-                    }
+                for (int j = 0; j < PART; ++j) {
+                    const int t = p % PARTS * PART + j;
+                    const v4i x = xf[p & 1][j];
+                    const uint32_t codes = wv[t % 2][g * SPG + t / 2];
+                    if constexpr (XT == DSQ_T_BF16)
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), codes_bf16(codes), acc, 0, 0, 0);
+                    else
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), codes_f16(codes), acc, 0, 0, 0);
+                }
                 facc[u & 1] = acc;
             }
-            if (u > 0) scaled(u - 1);
+            if (u > 0 && p % PARTS == 0) scaled(u - 1);
             __builtin_amdgcn_sched_barrier(0);
         }
         scaled(GPB * MT - 1);
     };
 
-    // Two sets of weight registers in turn (a copy of the prefetched set would wait for it): while a block is multiplied,
-    // the next one's rows and weights are under way.  What is fetched past the end is not used.
+    // Two sets of weight registers in turn (a copy of a prefetched set would wait for it), loaded again once their block is
+    // multiplied; the rows of the next block, of 8-bit ones of the one after it too, are under way meanwhile.  The loop runs an
+    // even number of blocks: what is fetched past the end meets scales of 0.
     v4u wa[2], wb[2];
     uint32_t sa[GPB], sb[GPB];
-    load_rows(0);
+    load_rows(0, xa);
     load_weights(0, wa, sa);
-    store_rows(0);
+    if (INT) load_rows(1, xb);
+    load_weights(1, wb, sb);
+    store_rows(0, xa);
     __syncthreads();
     for (int it = 0; it < iters; it += 2) {
-        load_rows(it + 1);
-        load_weights(it + 1, wb, sb);
+        load_rows(it + (INT ? 2 : 1), xa);
         __builtin_amdgcn_sched_barrier(0);
-        if (WK == 1 || it * WK + wk < KB) block(0, wa, sa);
-        if (it + 1 >= iters) break;
-        store_rows(1);
-        __syncthreads();
-        load_rows(it + 2);
+        block(0, wa, sa);
         load_weights(it + 2, wa, sa);
+        store_rows(1, INT ? xb : xa);
+        __syncthreads();
+        load_rows(it + (INT ? 3 : 2), xb);
         __builtin_amdgcn_sched_barrier(0);
-        if (WK == 1 || (it + 1) * WK + wk < KB) block(1, wb, sb);
-        if (it + 2 >= iters) break;
-        store_rows(0);
+        block(1, wb, sb);
+        load_weights(it + 3, wb, sb);
+        store_rows(0, INT ? xa : xb);
         __syncthreads();
     }
     if constexpr (WK > 1) {
@@ -286,7 +325,7 @@ template <int XT>
 hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 {
     const int64_t large = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
-    if (large >= 256) return launch_groups<XT, 4, 4, 1>(a, stream);
+    if (large >= 256) return launch_groups<XT, XT == DSQ_T_I8 ? 4 : 2, 4, 1>(a, stream);
     return launch_groups<XT, 2, 2, 4>(a, stream);
 }
 
