@@ -38,3 +38,7 @@ template <>
 struct Element<DSQ_T_BF16> {
     typedef __bf16 type;
 };
+template <>
+struct Element<DSQ_T_I8> {
+    typedef int8_t type;
+};

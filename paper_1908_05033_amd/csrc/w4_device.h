@@ -28,32 +28,29 @@ struct Frag<DSQ_T_I8> {
     long v;
 };
 
-// (WHOLE: channels k..k+7 exist.  Callers branch on the block and not here: behind a branch at each load it would be waited for.)
+// (WHOLE: channels k..k+7 exist.  Callers branch on the block and not here: behind a branch at each load it would be waited for.
+// A lane whose row does not exist keeps what `f` holds: rows of a matrix product do not meet.)
 template <int XT, bool WHOLE>
-__device__ __forceinline__ Frag<XT> load_frag(const void *row, int k, int K, bool live)
+__device__ __forceinline__ void load_frag(Frag<XT> &f, const void *row, int k, int K, bool live)
 {
-    Frag<XT> f = {};
+    if (!live) return;
     if constexpr (XT == DSQ_T_I8) {
         // (rows end with their pitch, a multiple of 128, and what lies behind K meets levels of 0)
-        if (live) f.v = *reinterpret_cast<const long *>((const int8_t *)row + k);
+        f.v = *reinterpret_cast<const long *>((const int8_t *)row + k);
     } else {
         typedef typename Element<XT>::type E;
-        const E *p = (const E *)row + k;
         if constexpr (WHOLE) {
-            if (live) {
-                const Side<E, 8> s = load_side<E, 8>(p);
+            const Side<E, 8> s = load_side<E, 8>((const E *)row + k);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f.v[i] = s.at[i];
-            }
-        } else if (live) {
+            for (int i = 0; i < 8; ++i) f.v[i] = s.at[i];
+        } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const E v = ((const E *)row)[k + i < K ? k + i : K - 1];
+                const E v = ((const E *)row)[k + i < K ? k + i : 0];
                 f.v[i] = k + i < K ? v : (E)0.0f;
             }
         }
     }
-    return f;
 }
 
 // The eight codes of a word as operand.
@@ -91,41 +88,49 @@ __device__ __forceinline__ void split3(const float (&x)[8], bf16x8 (&t)[3])
     }
 }
 
-// Adds the products of one step to a group's sums over a lane's four rows: acc for its output channel, xs those of x alone.
-template <int XT>
-struct Sums {
-    v4f acc, xs;
-};
-template <>
-struct Sums<DSQ_T_I8> {
-    v4i acc, xs;
-};
-
-template <int XT>
-__device__ __forceinline__ void step(uint32_t w, const Frag<XT> &x, Sums<XT> &s)
+// The sum over 4, 8 or 16 lanes side by side, in each of them: lanes exchanged by one and by two, then halves and rows of 16 mirrored.
+template <int CONTROL>
+__device__ __forceinline__ float plus_lane(float v)
 {
-    if constexpr (XT == DSQ_T_BF16) {
-        const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
-        s.acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, codes_bf16(w), s.acc, 0, 0, 0);
-        s.xs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, ones, s.xs, 0, 0, 0);
-    } else if constexpr (XT == DSQ_T_F16) {
-        const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
-        s.acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.v, codes_f16(w), s.acc, 0, 0, 0);
-        s.xs = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.v, ones, s.xs, 0, 0, 0);
-    } else if constexpr (XT == DSQ_T_F32) {
-        const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
-        bf16x8 t[3];
-        split3(x.v, t);
-        const bf16x8 c = codes_bf16(w);
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CONTROL, 0xF, 0xF, true));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v = plus_lane<0xB1>(v);
+    v = plus_lane<0x4E>(v);
+    if (LANES > 4) v = plus_lane<0x141>(v);
+    if (LANES > 8) v = plus_lane<0x140>(v);
+    return v;
+}
+
+// The sum of a lane's eight numbers.
+template <int XT>
+__device__ __forceinline__ float sum8(const Frag<XT> &f)
+{
+    float s = 0.0f;
+    if constexpr (XT == DSQ_T_F32) {
 #pragma unroll
-        for (int i = 2; i >= 0; --i) {
-            s.acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[i], c, s.acc, 0, 0, 0);
-            s.xs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[i], ones, s.xs, 0, 0, 0);
-        }
+        for (int i = 0; i < 8; ++i) s += f.v[i];
+    } else if constexpr (XT == DSQ_T_I8) {
+        const v2u v = __builtin_bit_cast(v2u, f.v);
+        const uint32_t lo = v.x, hi = v.y;
+        s = (float)__builtin_amdgcn_sdot4((int)lo, 0x01010101, __builtin_amdgcn_sdot4((int)hi, 0x01010101, 0, false), false);
     } else {
-        s.acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(x.v, codes_i8(w), s.acc, 0, 0, 0);
-        s.xs = __builtin_amdgcn_mfma_i32_16x16x32_i8(x.v, 0x0101010101010101L, s.xs, 0, 0, 0);
+        const v4u x = __builtin_bit_cast(v4u, f.v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = x[i];       // (a bit_cast of the vector's element itself takes element 0)
+            if constexpr (XT == DSQ_T_BF16) {
+                const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+                s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, s, false);
+            } else {
+                const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+                s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), ones, s, false);
+            }
+        }
     }
+    return s;
 }
 
 __device__ __forceinline__ float load_out(const void *p, int64_t i, int type)

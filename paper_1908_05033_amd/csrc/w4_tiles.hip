@@ -31,22 +31,6 @@ __device__ __forceinline__ void levels_i8(uint32_t w, uint32_t plus, int &lo, in
     hi = (int)((((w >> 4) & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
 }
 
-// The sum over 4, 8 or 16 lanes side by side, in each of them: lanes exchanged by one and by two, then halves and rows of 16 mirrored.
-template <int CONTROL>
-__device__ __forceinline__ float plus_lane(float v)
-{
-    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CONTROL, 0xF, 0xF, true));
-}
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v)
-{
-    v = plus_lane<0xB1>(v);
-    v = plus_lane<0x4E>(v);
-    if (LANES > 4) v = plus_lane<0x141>(v);
-    if (LANES > 8) v = plus_lane<0x140>(v);
-    return v;
-}
-
 // Results of a wave's tile of 32 rows: row 8 * (c / 4) + 4h + c % 4, the lane's channel n.
 template <int XT, int OT>
 __device__ __forceinline__ void store_tile(const DsqW4Args &a, const v16f &sum, int64_t m0, int n, int h)
@@ -118,7 +102,8 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 // (blocks past the last one meet no weights)
                 xr[j] = *reinterpret_cast<const v4u *>((const char *)a.x + m * a.x_stride + 128 * (b < KB ? b : KB - 1) + 16 * unit);
             } else {
-                const Frag<XT> f = load_frag<XT, whole.value>((const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
+                Frag<XT> f;
+                load_frag<XT, whole.value>(f, (const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
                 xr[j] = __builtin_bit_cast(v4u, f.v);
             }
         }
@@ -134,18 +119,9 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             *reinterpret_cast<v4u *>(lds + (to * WK + k) * BLOCK + row * L::PITCH + 16 * unit) = xr[j];
             if constexpr (!INT) {
                 // the sum of a group of x: eight channels a lane, 4 * SPG lanes side by side
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t pair = xr[j][i];       // (a bit_cast of the vector's element itself takes element 0)
-                    if constexpr (XT == DSQ_T_BF16) {
-                        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-                        s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, s, false);
-                    } else {
-                        const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
-                        s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), ones, s, false);
-                    }
-                }
+                Frag<XT> f;
+                f.v = __builtin_bit_cast(decltype(f.v), xr[j]);
+                float s = sum8(f);
                 s = lanes_sum<4 * SPG>(s);
                 if (unit % (4 * SPG) == 0) xsums[(to * WK + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
             }
@@ -326,6 +302,7 @@ hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 {
     const int64_t large = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
     if (large >= 256) return launch_groups<XT, XT == DSQ_T_I8 ? 4 : 2, 4, 1>(a, stream);
+    if (a.M <= 32) return launch_groups<XT, 1, 2, 4>(a, stream);
     return launch_groups<XT, 2, 2, 4>(a, stream);
 }
 
