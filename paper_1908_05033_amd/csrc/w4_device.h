@@ -43,6 +43,14 @@ __device__ __forceinline__ void load_frag(Frag<XT> &f, const void *row, int k, i
             const Side<E, 8> s = load_side<E, 8>((const E *)row + k);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f.v[i] = s.at[i];
+        } else if (sizeof(E) == 2 && K >= 8) {
+            // the row's last eight, moved down by as many as lie before k
+            const int back = k + 8 - K, n = 16 * (back < 0 ? 0 : back > 8 ? 8 : back);
+            const Side<uint64_t, 2> s = load_side<uint64_t, 2>((const uint64_t *)((const E *)row + (back > 0 ? K - 8 : k)));
+            const uint64_t lo = s.at[0], hi = s.at[1];
+            const uint64_t to[2] = {n == 0 ? lo : n < 64 ? lo >> n | hi << (64 - n) : n < 128 ? hi >> (n - 64) : 0,
+                                    n < 64 ? hi >> n : 0};
+            __builtin_memcpy(&f, to, 16);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {

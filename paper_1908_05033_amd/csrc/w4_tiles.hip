@@ -109,8 +109,14 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
         }
     };
     auto load_rows = [&](int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
-        if (INT || 128 * WK * (it + 1) <= a.K) load_as(it, xr, std::true_type());
-        else load_as(it, xr, std::false_type());
+        if (it >= iters) {                                            // (meets scales of 0: any number will do)
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) xr[j] = (v4u){0u, 0u, 0u, 0u};
+        } else if (INT || 128 * WK * (it + 1) <= a.K) {
+            load_as(it, xr, std::true_type());
+        } else {
+            load_as(it, xr, std::false_type());
+        }
     };
     auto store_rows = [&](int to, const v4u (&xr)[LOADS]) __attribute__((always_inline)) {
 #pragma unroll
