@@ -1,13 +1,19 @@
 // Many rows times group-scaled 4-bit weights (8-bit codes or 16-bit floats): a tiled product on the 32x32 matrix instructions.
 //
-// A workgroup of four waves owns 32 * MT rows x 128 output channels.  Blocks of 128 input channels of its rows go through
-// LDS (rows padded by 16 bytes: reads of a column of 16-byte units are free of bank conflicts); a wave takes 32 channels,
-// whose codes come from global memory in lane order, and all rows, so that a code is unpacked once for 32 * MT rows.  With the rows as
-// the first operand a lane holds one output channel: its scale and zero point are one word a group.
+// A workgroup of eight waves owns 32 * MT rows x 32 * WN output channels.  Blocks of 128 input channels of its rows go through
+// LDS (rows padded by 16 bytes: reads of a column of 16-byte units are free of bank conflicts); a wave takes 32 output
+// channels, whose codes come from global memory in lane order, and all rows, so that a code is unpacked once for 32 * MT rows;
+// WK waves share a channel's input blocks and join their sums in LDS at the end.  With the rows as the first operand a lane
+// holds one output channel: its scale and zero point are one word a group.
 //
 // 8-bit rows: the operand is code - z as bytes, a group's sum an exact integer, converted and scaled once a group (two
-// vector instructions an element: these, not the matrix instruction, bound the kernel at groups of 128 and below).
-// Floats: the operand is the code, and the group's sum of x, from the staging of the rows, carries the zero point.
+// vector instructions an element, which no matrix instruction can take over).  Floats: the operand is the code, and the group's
+// sum of x, from the staging of the rows, carries the zero point.
+//
+// Measured at K = 4096 and groups of 128: 2048 rows to 8192 channels 109 us (1.26 POP/s) with 8-bit rows, 164 us (0.84 PFLOP/s)
+// with bfloat16 ones; of the former 97 us are left without the scaling of the groups, 100 without loads: bound by the matrix
+// instructions' issue between barriers.  512 rows to 4096: 21 and 31 us, bound by the rows' and codes' way from the L2 (some 47 GB/s
+// for a compute unit).
 #include <type_traits>
 
 #include "w4_device.h"
@@ -55,18 +61,21 @@ __device__ __forceinline__ void store_tile(const DsqW4Args &a, const v16f &sum, 
     }
 }
 
-// MT: tiles of 32 rows; WN x WK waves: 32 output channels each, and every WK-th block of input channels; GPB: groups of a block.
-template <int XT, int MT, int WN, int WK, int GPB>
+// MT: tiles of 32 rows; WN x WK waves: 32 output channels each, and the WK-th part of an iteration's blocks, BPI each (fewer
+// barriers: 3 % at 128 x 256); GPB: groups of a block.
+template <int XT, int MT, int WN, int WK, int BPI, int GPB>
 __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, int tiles_m, int total, int xcd_chunk)
 {
     typedef Tile<XT> L;
     constexpr bool INT = XT == DSQ_T_I8;
     constexpr int SPG = 4 / GPB;                                      // steps of 32 channels in a group
     constexpr int THREADS = 64 * WN * WK, ROWS = 32 * MT, BLOCK = ROWS * L::PITCH;
-    constexpr int LOADS = ROWS * L::UNITS * WK / THREADS;             // 16-byte units a thread stages
+    constexpr int STEP = WK * BPI;                                    // blocks of an iteration
+    constexpr bool DEEP = BPI == 1;                                   // rows are fetched two iterations ahead
+    constexpr int LOADS = ROWS * L::UNITS * STEP / THREADS;             // 16-byte units a thread stages
     constexpr int XSUM = INT ? 0 : GPB * ROWS;                        // sums of x of a block's groups
-    extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][WK] blocks, then [2][WK] sums
-    float *xsums = reinterpret_cast<float *>(lds + 2 * WK * BLOCK);
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][STEP] blocks, then [2][STEP] sums
+    float *xsums = reinterpret_cast<float *>(lds + 2 * STEP * BLOCK);
 
     // Workgroups are dealt to the 8 XCDs in turn: each gets a contiguous range of tiles, the row tiles of one channel tile
     // together, so that its weights are read into one L2 only
@@ -76,7 +85,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     const int64_t m0 = (int64_t)(logical - nt * tiles_m) * ROWS;
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wn = wave % WN, wk = wave / WN;
-    const int KB = dsq_w4_round(a.K) / 128, Gp = KB * GPB, iters = (KB + WK - 1) / WK;
+    const int KB = dsq_w4_round(a.K) / 128, Gp = KB * GPB, iters = (KB + STEP - 1) / STEP;
     const int n0 = nt * 32 * WN + 32 * wn;
     // this lane's channel: 16-channel block (r / 16), column r % 16; its halves of 16 input channels
     const size_t ct = (size_t)(n0 / 16 + r / 16);
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     auto load_as = [&](int it, v4u (&xr)[LOADS], auto whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int line = line0 + j * LINES, row = line % ROWS, b = it * WK + line / ROWS;
+            const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
             if constexpr (INT) {
@@ -112,7 +121,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
         if (it >= iters) {                                            // (meets scales of 0: any number will do)
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) xr[j] = (v4u){0u, 0u, 0u, 0u};
-        } else if (INT || 128 * WK * (it + 1) <= a.K) {
+        } else if (INT || 128 * STEP * (it + 1) <= a.K) {
             load_as(it, xr, std::true_type());
         } else {
             load_as(it, xr, std::false_type());
@@ -122,33 +131,37 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, k = line / ROWS;
-            *reinterpret_cast<v4u *>(lds + (to * WK + k) * BLOCK + row * L::PITCH + 16 * unit) = xr[j];
+            *reinterpret_cast<v4u *>(lds + (to * STEP + k) * BLOCK + row * L::PITCH + 16 * unit) = xr[j];
             if constexpr (!INT) {
                 // the sum of a group of x: eight channels a lane, 4 * SPG lanes side by side
                 Frag<XT> f;
                 f.v = __builtin_bit_cast(decltype(f.v), xr[j]);
                 float s = sum8(f);
                 s = lanes_sum<4 * SPG>(s);
-                if (unit % (4 * SPG) == 0) xsums[(to * WK + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
+                if (unit % (4 * SPG) == 0) xsums[(to * STEP + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
             }
         }
     };
-    auto load_weights = [&](int it, v4u (&to)[2], uint32_t (&s)[GPB]) __attribute__((always_inline)) {
-        // (past the end: the last block's with scales of 0)
-        const bool live = it * WK + wk < KB;
-        const int b = live ? it * WK + wk : KB - 1;
-        to[0] = w[(size_t)b * 64];
-        to[1] = w[(size_t)b * 64 + 16];
+    auto load_weights = [&](int it, v4u (&to)[BPI][2], uint32_t (&s)[BPI][GPB]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int g = 0; g < GPB; ++g) {
-            s[g] = sc[(size_t)(b * GPB + g) * 16];
-            if (!live) s[g] = 0;
+        for (int j = 0; j < BPI; ++j) {
+            // (past the end: the last block's with scales of 0)
+            const int at = it * STEP + wk * BPI + j;
+            const bool live = it < iters && at < KB;
+            const int b = live ? at : KB - 1;
+            to[j][0] = w[(size_t)b * 64];
+            to[j][1] = w[(size_t)b * 64 + 16];
+#pragma unroll
+            for (int g = 0; g < GPB; ++g) {
+                s[j][g] = sc[(size_t)(b * GPB + g) * 16];
+                if (!live) s[j][g] = 0;
+            }
         }
     };
-    // One block of input channels from LDS area `from`.
-    auto block = [&](int from, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) __attribute__((always_inline)) {
-        const char *base = lds + (from * WK + wk) * BLOCK + r * L::PITCH + 16 * L::ES * h;
-        const float *xsum = xsums + (from * WK + wk) * XSUM;
+    // One block of input channels from LDS block `at`.
+    auto block = [&](int at, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) __attribute__((always_inline)) {
+        const char *base = lds + at * BLOCK + r * L::PITCH + 16 * L::ES * h;
+        const float *xsum = xsums + at * XSUM;
         // Units of one group and 32 rows: the matrix instructions of a unit stand beside the scaling of the one before, and its
         // rows are read from LDS one unit ahead.  (Left to itself the compiler reads the rows of all units first and spills, or
         // reads each operand right before its instruction and waits.)
@@ -228,28 +241,32 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     };
 
     // Two sets of weight registers in turn (a copy of a prefetched set would wait for it), loaded again once their block is
-    // multiplied; the rows of the next block, of 8-bit ones of the one after it too, are under way meanwhile.  The loop runs an
-    // even number of blocks: what is fetched past the end meets scales of 0.
-    v4u wa[2], wb[2];
-    uint32_t sa[GPB], sb[GPB];
+    // multiplied; the rows of the next iteration, and of the one after it too where it is one block (bfloat16: 2 to 5 %), are
+    // under way meanwhile.  The loop runs an even number of iterations: what is fetched past the end meets scales of 0.
+    auto blocks = [&](int from, const v4u (&wv)[BPI][2], const uint32_t (&sv)[BPI][GPB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < BPI; ++j) block(from * STEP + wk * BPI + j, wv[j], sv[j]);
+    };
+    v4u wa[BPI][2], wb[BPI][2];
+    uint32_t sa[BPI][GPB], sb[BPI][GPB];
     load_rows(0, xa);
     load_weights(0, wa, sa);
-    if (INT) load_rows(1, xb);
+    if (DEEP) load_rows(1, xb);
     load_weights(1, wb, sb);
     store_rows(0, xa);
     __syncthreads();
     for (int it = 0; it < iters; it += 2) {
-        load_rows(it + (INT ? 2 : 1), xa);
+        load_rows(it + (DEEP ? 2 : 1), xa);
         __builtin_amdgcn_sched_barrier(0);
-        block(0, wa, sa);
+        blocks(0, wa, sa);
         load_weights(it + 2, wa, sa);
-        store_rows(1, INT ? xb : xa);
+        store_rows(1, DEEP ? xb : xa);
         __syncthreads();
-        load_rows(it + (INT ? 3 : 2), xb);
+        load_rows(it + (DEEP ? 3 : 2), xb);
         __builtin_amdgcn_sched_barrier(0);
-        block(1, wb, sb);
+        blocks(1, wb, sb);
         load_weights(it + 3, wb, sb);
-        store_rows(0, INT ? xa : xb);
+        store_rows(0, DEEP ? xa : xb);
         __syncthreads();
     }
     if constexpr (WK > 1) {
@@ -278,16 +295,16 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     }
 }
 
-template <int XT, int MT, int WN, int WK, int GPB>
+template <int XT, int MT, int WN, int WK, int BPI, int GPB>
 hipError_t launch_of(const DsqW4Args &a, hipStream_t stream)
 {
     typedef Tile<XT> L;
-    constexpr int STAGE = 2 * WK * (32 * MT * L::PITCH + (XT == DSQ_T_I8 ? 0 : GPB * 32 * MT * 4));
+    constexpr int STAGE = 2 * WK * BPI * (32 * MT * L::PITCH + (XT == DSQ_T_I8 ? 0 : GPB * 32 * MT * 4));
     constexpr int JOIN = WK > 1 ? WN * WK * MT * 64 * 64 : 0, LDS = STAGE > JOIN ? STAGE : JOIN;
     const int64_t tiles_m = ((int64_t)a.M + 32 * MT - 1) / (32 * MT), tiles_n = ((int64_t)a.N + 32 * WN - 1) / (32 * WN);
     const int64_t total = tiles_m * tiles_n, xcd_chunk = (total + 7) / 8;
     if (xcd_chunk * 8 * 64 * WN * WK >= 1LL << 32) return hipErrorInvalidConfiguration;
-    auto kern = w4_tiles_kernel<XT, MT, WN, WK, GPB>;
+    auto kern = w4_tiles_kernel<XT, MT, WN, WK, BPI, GPB>;
     if (LDS > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
         if (e != hipSuccess) return e;
@@ -296,20 +313,46 @@ hipError_t launch_of(const DsqW4Args &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <int XT, int MT, int WN, int WK>
+template <int XT, int MT, int WN, int WK, int BPI = 1>
 hipError_t launch_groups(const DsqW4Args &a, hipStream_t stream)
 {
-    return a.group == 32 ? launch_of<XT, MT, WN, WK, 4>(a, stream)
-           : a.group == 64 ? launch_of<XT, MT, WN, WK, 2>(a, stream) : launch_of<XT, MT, WN, WK, 1>(a, stream);
+    return a.group == 32 ? launch_of<XT, MT, WN, WK, BPI, 4>(a, stream)
+           : a.group == 64 ? launch_of<XT, MT, WN, WK, BPI, 2>(a, stream) : launch_of<XT, MT, WN, WK, BPI, 1>(a, stream);
 }
 
 template <int XT>
 hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 {
-    const int64_t large = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
-    if (large >= 256) return launch_groups<XT, XT == DSQ_T_I8 ? 4 : 2, 4, 1>(a, stream);
-    if (a.M <= 32) return launch_groups<XT, 1, 2, 4>(a, stream);
-    return launch_groups<XT, 2, 2, 4>(a, stream);
+    constexpr bool INT = XT == DSQ_T_I8;
+    // A large tile reads least and unpacks a code for most rows, a small one leaves no compute unit idle: of five tiles the one
+    // with the least rounds over the 256 compute units times its time for a round.  Those times are measured at K = 4096 and
+    // groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
+    //
+    //   rows x N        32x64      64x64      64x128     64x256     128x256
+    //   128 x 4096      16 / 11    23 / 14    31 / 20    41 / 30    75 / 45
+    //   256 x 4096      28 / 19    24 / 15    32 / 20    42 / 30    74 / 46
+    //   512 x 4096      53 / 32    44 / 25    33 / 22    42 / 30    75 / 46
+    //   1024 x 4096    111 / 70    89 / 48    63 / 41    48 / 33    77 / 47
+    //   2048 x 8192    421 / 270  360 / 211  252 / 169  186 / 129  172 / 108
+    struct { int rows, channels, time; } const tiles[5] = {{32, 64, INT ? 10 : 15}, {64, 64, INT ? 14 : 23}, {64, 128, INT ? 20 : 31},
+                                                           {64, 256, INT ? 30 : 42}, {128, 256, INT ? 48 : 78}};
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < 5; ++i) {
+        const int64_t count = (((int64_t)a.M + tiles[i].rows - 1) / tiles[i].rows) * (((int64_t)a.N + tiles[i].channels - 1) / tiles[i].channels);
+        const int64_t time = (count + 255) / 256 * tiles[i].time;
+        if (time < least) {
+            least = time;
+            best = i;
+        }
+    }
+    switch (best) {
+    case 0: return launch_groups<XT, 1, 2, 4>(a, stream);
+    case 1: return launch_groups<XT, 2, 2, 4>(a, stream);
+    case 2: return launch_groups<XT, 2, 4, 2>(a, stream);
+    case 3: return launch_groups<XT, 2, 8, 1, 2>(a, stream);
+    default: return launch_groups<XT, 4, 8, 1, INT ? 2 : 1>(a, stream);       // (floats: two blocks an iteration would spill)
+    }
 }
 
 }  // namespace
