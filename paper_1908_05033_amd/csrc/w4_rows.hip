@@ -209,6 +209,7 @@ hipError_t dsq_launch_w4_rows(const DsqW4Args &a, hipStream_t stream)
 hipError_t dsq_launch_w4_linear(const DsqW4Args &a, hipStream_t stream)
 {
     if (a.M == 1) return dsq_launch_w4_row(a, stream);
-    if (a.M > 16 && a.x_type != DSQ_T_F32) return dsq_launch_w4_tiles(a, stream);
+    // (the tiles take rows of floats 16 bytes at a time)
+    if (a.M > 16 && (a.x_type == DSQ_T_I8 || (a.x_type != DSQ_T_F32 && a.K >= 8))) return dsq_launch_w4_tiles(a, stream);
     return dsq_launch_w4_rows(a, stream);
 }

@@ -10,10 +10,10 @@
 // vector instructions an element, which no matrix instruction can take over).  Floats: the operand is the code, and the group's
 // sum of x, from the staging of the rows, carries the zero point.
 //
-// Measured at K = 4096 and groups of 128: 2048 rows to 8192 channels 109 us (1.26 POP/s) with 8-bit rows, 164 us (0.84 PFLOP/s)
-// with bfloat16 ones; of the former 97 us are left without the scaling of the groups, 100 without loads: bound by the matrix
-// instructions' issue between barriers.  512 rows to 4096: 21 and 31 us, bound by the rows' and codes' way from the L2 (some 47 GB/s
-// for a compute unit).
+// Measured at K = 4096 and groups of 128: 2048 rows to 8192 channels 107 us (1.28 POP/s) with 8-bit rows, 158 us (0.87
+// PFLOP/s) with bfloat16 ones, bound by the matrix instructions' issue between barriers and the scaling beside it.  256 rows to 4096: 14
+// and 22 us.  Of the latter a call without work is 6, and for its 16 million codes the loads alone, the writes to LDS alone and the
+// multiplication alone would take 8, 4 and 10: they overlap in part only, with one workgroup on a compute unit.
 #include <type_traits>
 
 #include "w4_device.h"
@@ -35,30 +35,6 @@ __device__ __forceinline__ void levels_i8(uint32_t w, uint32_t plus, int &lo, in
 {
     lo = (int)(((w & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
     hi = (int)((((w >> 4) & 0x0F0F0F0Fu) + plus) ^ 0x80808080u);
-}
-
-// Results of a wave's tile of 32 rows: row 8 * (c / 4) + 4h + c % 4, the lane's channel n.
-template <int XT, int OT>
-__device__ __forceinline__ void store_tile(const DsqW4Args &a, const v16f &sum, int64_t m0, int n, int h)
-{
-    typedef typename Element<OT>::type E;
-    if (n >= a.N) return;
-    const float bias = a.bias ? (float)((const E *)a.bias)[n] : 0.0f;
-    E *out = (E *)a.out + n;
-    float scale[16];
-    if constexpr (XT == DSQ_T_I8)
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-            const int64_t m = m0 + 8 * (c / 4) + 4 * h + c % 4;
-            scale[c] = a.x_scale[m < a.M ? m : a.M - 1];
-        }
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        const int64_t m = m0 + 8 * (c / 4) + 4 * h + c % 4;
-        float o = XT == DSQ_T_I8 ? sum[c] * scale[c] : sum[c];
-        if (a.bias) o += bias;
-        if (m < a.M) out[m * a.out_stride] = (E)o;
-    }
 }
 
 // MT: tiles of 32 rows; WN x WK waves: 32 output channels each, and the WK-th part of an iteration's blocks, BPI each (fewer
@@ -101,33 +77,41 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     const int unit = threadIdx.x % L::UNITS, line0 = threadIdx.x / L::UNITS;
     constexpr int LINES = THREADS / L::UNITS;                         // rows a load instruction of the workgroup covers
     v4u xa[LOADS], xb[LOADS];
-    auto load_as = [&](int it, v4u (&xr)[LOADS], auto whole) __attribute__((always_inline)) {
+    auto load_rows = [&](int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
+        if (it >= iters) {                                            // (meets scales of 0: any number will do)
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) xr[j] = (v4u){0u, 0u, 0u, 0u};
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
-            if constexpr (INT) {
-                // (blocks past the last one meet no weights)
-                xr[j] = *reinterpret_cast<const v4u *>((const char *)a.x + m * a.x_stride + 128 * (b < KB ? b : KB - 1) + 16 * unit);
-            } else {
-                Frag<XT> f;
-                load_frag<XT, whole.value>(f, (const char *)a.x + m * a.x_stride * 2, 128 * b + 8 * unit, a.K, true);
-                xr[j] = __builtin_bit_cast(v4u, f.v);
-            }
+            // past the row's end its last 16 bytes: of blocks that meet no weights or scales of 0, or cut off by `cut`
+            const int k = 128 * b + 16 / L::ES * unit, last = (INT ? 128 * KB : a.K) - 16 / L::ES;
+            xr[j] = load_side<v4u, 1>((const v4u *)((const char *)a.x + m * a.x_stride * L::ES + (int64_t)(k < last ? k : last) * L::ES)).at[0];
         }
     };
-    auto load_rows = [&](int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
-        if (it >= iters) {                                            // (meets scales of 0: any number will do)
+    // Floats of the last block, k..k+7 of a row of K: moved down by as many as lie before k, zeros behind K.
+    auto cut = [&](const v4u &x, int k) __attribute__((always_inline)) {
+        const int back = k + 8 - a.K, n = 16 * (back < 0 ? 0 : back > 8 ? 8 : back);
+        uint64_t at[2];
+        __builtin_memcpy(at, &x, 16);
+        const uint64_t lo = n >= 128 ? 0 : n >= 64 ? at[1] : at[0], hi = n >= 64 ? 0 : at[1];
+        const uint64_t to[2] = {lo >> (n & 63) | hi << 1 << (63 - (n & 63)), hi >> (n & 63)};
+        v4u y;
+        __builtin_memcpy(&y, to, 16);
+        return y;
+    };
+    const int it_cut = !INT && a.K % 128 ? iters - 1 : -1;
+    auto store_rows = [&](int to, int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
+        if (!INT && it == it_cut)
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) xr[j] = (v4u){0u, 0u, 0u, 0u};
-        } else if (INT || 128 * STEP * (it + 1) <= a.K) {
-            load_as(it, xr, std::true_type());
-        } else {
-            load_as(it, xr, std::false_type());
-        }
-    };
-    auto store_rows = [&](int to, const v4u (&xr)[LOADS]) __attribute__((always_inline)) {
+            for (int j = 0; j < LOADS; ++j) {
+                xr[j] = cut(xr[j], 128 * (it * STEP + (line0 + j * LINES) / ROWS) + 8 * unit);
+                __builtin_amdgcn_sched_barrier(0);                    // (one after the other: side by side they spill)
+            }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, k = line / ROWS;
@@ -253,46 +237,77 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     load_weights(0, wa, sa);
     if (DEEP) load_rows(1, xb);
     load_weights(1, wb, sb);
-    store_rows(0, xa);
+    store_rows(0, 0, xa);
     __syncthreads();
     for (int it = 0; it < iters; it += 2) {
         load_rows(it + (DEEP ? 2 : 1), xa);
         __builtin_amdgcn_sched_barrier(0);
         blocks(0, wa, sa);
         load_weights(it + 2, wa, sa);
-        store_rows(1, DEEP ? xb : xa);
+        store_rows(1, it + 1, DEEP ? xb : xa);
         __syncthreads();
         load_rows(it + (DEEP ? 3 : 2), xb);
         __builtin_amdgcn_sched_barrier(0);
         blocks(1, wb, sb);
         load_weights(it + 3, wb, sb);
-        store_rows(0, DEEP ? xa : xb);
+        store_rows(0, it + 2, DEEP ? xa : xb);
         __syncthreads();
     }
+    // Registers 4q..4q+3 of a lane are rows 8q + 4h + 0..3 of a tile of 32: the WK waves of a channel tile leave their sums in
+    // LDS, and each joins and stores the quarters q of its own.
+    v4f *part = reinterpret_cast<v4f *>(lds);                         // [wave][row tile][quarter][lane]
     if constexpr (WK > 1) {
-        // the waves of a channel tile join their sums
         __syncthreads();
-        v16f *part = reinterpret_cast<v16f *>(lds);                   // [wave][row tile][lane]
 #pragma unroll
-        for (int i = 0; i < MT; ++i) part[(wave * MT + i) * 64 + lane] = sum[i];
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                part[((wave * MT + i) * 4 + q) * 64 + lane] = (v4f){sum[i][4 * q], sum[i][4 * q + 1], sum[i][4 * q + 2], sum[i][4 * q + 3]};
         __syncthreads();
+    }
+    const int n = n0 + r;
+    if (n >= a.N) return;
+    constexpr int QS = 4 / WK;                                        // quarters of a tile that a wave stores
+    auto store = [&](auto type) __attribute__((always_inline)) {
+        typedef decltype(type) E;
+        const float bias = a.bias ? (float)((const E *)a.bias)[n] : 0.0f;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            if (i % WK != wk) continue;
-            sum[i] = part[(wn * MT + i) * 64 + lane];
+            const int64_t m = m0 + 32 * i + 8 * wk + 4 * h;           // the lane's first row of the tile
+            const int live = a.M - m < 32 ? (int)(a.M - m) : 32;
+            if (live <= 0) return;
+            float scale[4 * QS];
+            if constexpr (INT)
 #pragma unroll
-            for (int k = 1; k < WK; ++k) sum[i] += part[((k * WN + wn) * MT + i) * 64 + lane];
+                for (int c = 0; c < 4 * QS; ++c) {
+                    const int at = 8 * WK * (c / 4) + c % 4;
+                    scale[c] = a.x_scale[m + (at < live ? at : 0)];
+                }
+            E *out = (E *)a.out + m * a.out_stride + n;
+#pragma unroll
+            for (int j = 0; j < QS; ++j) {
+                v4f s;
+                if constexpr (WK > 1) {
+                    const int q = j * WK + wk;
+                    s = part[((wn * MT + i) * 4 + q) * 64 + lane];
+#pragma unroll
+                    for (int k = 1; k < WK; ++k) s += part[(((k * WN + wn) * MT + i) * 4 + q) * 64 + lane];
+                } else {
+                    s = (v4f){sum[i][4 * j], sum[i][4 * j + 1], sum[i][4 * j + 2], sum[i][4 * j + 3]};
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float o = INT ? s[c] * scale[4 * j + c] : s[c];
+                    if (a.bias) o += bias;
+                    if (8 * WK * j + c < live) out[(8 * WK * j + c) * a.out_stride] = (E)o;
+                }
+            }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        if (WK > 1 && i % WK != wk) continue;
-        const int64_t m = m0 + 32 * i;
-        if (!INT) store_tile<XT, INT ? DSQ_T_F32 : XT>(a, sum[i], m, n0 + r, h);
-        else if (a.out_type == DSQ_T_BF16) store_tile<XT, DSQ_T_BF16>(a, sum[i], m, n0 + r, h);
-        else if (a.out_type == DSQ_T_F16) store_tile<XT, DSQ_T_F16>(a, sum[i], m, n0 + r, h);
-        else store_tile<XT, DSQ_T_F32>(a, sum[i], m, n0 + r, h);
-    }
+    };
+    if constexpr (!INT) store((typename Element<INT ? DSQ_T_F32 : XT>::type)0.0f);
+    else if (a.out_type == DSQ_T_BF16) store((__bf16)0.0f);
+    else if (a.out_type == DSQ_T_F16) store((_Float16)0.0f);
+    else store(0.0f);
 }
 
 template <int XT, int MT, int WN, int WK, int BPI, int GPB>
@@ -329,13 +344,13 @@ hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
     // groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
     //
     //   rows x N        32x64      64x64      64x128     64x256     128x256
-    //   128 x 4096      16 / 11    23 / 14    31 / 20    41 / 30    75 / 45
-    //   256 x 4096      28 / 19    24 / 15    32 / 20    42 / 30    74 / 46
-    //   512 x 4096      53 / 32    44 / 25    33 / 22    42 / 30    75 / 46
-    //   1024 x 4096    111 / 70    89 / 48    63 / 41    48 / 33    77 / 47
-    //   2048 x 8192    421 / 270  360 / 211  252 / 169  186 / 129  172 / 108
-    struct { int rows, channels, time; } const tiles[5] = {{32, 64, INT ? 10 : 15}, {64, 64, INT ? 14 : 23}, {64, 128, INT ? 20 : 31},
-                                                           {64, 256, INT ? 30 : 42}, {128, 256, INT ? 48 : 78}};
+    //   128 x 4096      13 / 10    20 / 13    25 / 19    37 / 29    63 / 44
+    //   256 x 4096      25 / 13    22 / 14    26 / 20    37 / 29    62 / 44
+    //   512 x 4096      45 / 24    40 / 24    28 / 21    38 / 30    63 / 45
+    //   1024 x 4096    103 / 49    77 / 48    56 / 41    45 / 33    66 / 46
+    //   2048 x 8192    388 / 198  324 / 221  226 / 165  184 / 129  157 / 108
+    struct { int rows, channels, time; } const tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 13 : 20}, {64, 128, INT ? 20 : 27},
+                                                           {64, 256, INT ? 30 : 41}, {128, 256, INT ? 48 : 76}};
     int best = 0;
     int64_t least = INT64_MAX;
     for (int i = 0; i < 5; ++i) {
