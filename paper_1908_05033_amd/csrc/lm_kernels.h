@@ -63,7 +63,6 @@ struct DsqW4Args {
     int x_type, out_type;
 };
 hipError_t dsq_launch_w4_linear(const DsqW4Args &a, hipStream_t stream);
-// The kernels for one row, for a few rows and for many rows (8-bit and 16-bit ones).
+// The kernels for one row and for a few rows; those for many stand beside the choice.
 hipError_t dsq_launch_w4_row(const DsqW4Args &a, hipStream_t stream);
 hipError_t dsq_launch_w4_rows(const DsqW4Args &a, hipStream_t stream);
-hipError_t dsq_launch_w4_tiles(const DsqW4Args &a, hipStream_t stream);

@@ -1,4 +1,4 @@
-// A few rows times group-scaled 4-bit weights, and the choice of the kernel for a number of rows.
+// A few rows times group-scaled 4-bit weights.
 //
 // As in w4_row.hip a wave owns output channels and a share of the blocks of 128 input channels; the waves of a workgroup
 // join their sums in LDS, in a fixed order.  Each wave reads the rows of its blocks straight into the operands' registers: its
@@ -169,13 +169,24 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(DsqW4Args a)
 }
 
 template <int XT, int NT, int CHUNK>
-hipError_t launch_rows(const DsqW4Args &a, hipStream_t stream)
+hipError_t launch_rows(DsqW4Args a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((a.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.M + 15) / 16));
-    if (a.group == 32) w4_rows_kernel<XT, NT, CHUNK, 4><<<grid, 64 * WAVES, 0, stream>>>(a);
-    else if (a.group == 64) w4_rows_kernel<XT, NT, CHUNK, 2><<<grid, 64 * WAVES, 0, stream>>>(a);
-    else w4_rows_kernel<XT, NT, CHUNK, 1><<<grid, 64 * WAVES, 0, stream>>>(a);
-    return hipGetLastError();
+    const int64_t tiles_n = ((int64_t)a.N + 16 * NT - 1) / (16 * NT), out_size = a.out_type == DSQ_T_F32 ? 4 : 2;
+    // (a launch holds under 2^32 threads and 2^16 workgroups in its second dimension)
+    const int most = (int)((1 << 22) / tiles_n < 32768 ? (1 << 22) / tiles_n : 32768) * 16;
+    for (int left = a.M; left > 0; left -= most) {
+        a.M = left < most ? left : most;
+        const dim3 grid((unsigned)tiles_n, (unsigned)((a.M + 15) / 16));
+        if (a.group == 32) w4_rows_kernel<XT, NT, CHUNK, 4><<<grid, 64 * WAVES, 0, stream>>>(a);
+        else if (a.group == 64) w4_rows_kernel<XT, NT, CHUNK, 2><<<grid, 64 * WAVES, 0, stream>>>(a);
+        else w4_rows_kernel<XT, NT, CHUNK, 1><<<grid, 64 * WAVES, 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.x = (const char *)a.x + most * a.x_stride * (int64_t)sizeof(typename Element<XT>::type);
+        a.out = (char *)a.out + most * a.out_stride * out_size;
+        if (XT == DSQ_T_I8) a.x_scale += most;
+    }
+    return hipSuccess;
 }
 
 template <int XT>
@@ -204,12 +215,4 @@ hipError_t dsq_launch_w4_rows(const DsqW4Args &a, hipStream_t stream)
     case DSQ_T_BF16: return launch_of<DSQ_T_BF16>(a, stream);
     }
     return launch_of<DSQ_T_I8>(a, stream);
-}
-
-hipError_t dsq_launch_w4_linear(const DsqW4Args &a, hipStream_t stream)
-{
-    if (a.M == 1) return dsq_launch_w4_row(a, stream);
-    // (the tiles take rows of floats 16 bytes at a time)
-    if (a.M > 16 && (a.x_type == DSQ_T_I8 || (a.x_type != DSQ_T_F32 && a.K >= 8))) return dsq_launch_w4_tiles(a, stream);
-    return dsq_launch_w4_rows(a, stream);
 }

@@ -1,4 +1,4 @@
-// Many rows times group-scaled 4-bit weights (8-bit codes or 16-bit floats): a tiled product on the 32x32 matrix instructions.
+// Many rows times group-scaled 4-bit weights: a tiled product on the 32x32 matrix instructions; the choice of kernel and tile.
 //
 // A workgroup of eight waves owns 32 * MT rows x 32 * WN output channels.  Blocks of 128 input channels of its rows go through
 // LDS (rows padded by 16 bytes: reads of a column of 16-byte units are free of bank conflicts); a wave takes 32 output
@@ -25,9 +25,12 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 
 template <int XT>
 struct Tile {
-    static constexpr int ES = XT == DSQ_T_I8 ? 1 : 2;
-    static constexpr int ROW = 128 * ES, PITCH = ROW + 16;            // bytes of a block's row in LDS
-    static constexpr int UNITS = ROW / 16;                            // 16-byte units of a row
+    static constexpr int ES = sizeof(typename Element<XT>::type);
+    static constexpr int PLANES = XT == DSQ_T_F32 ? 3 : 1;            // a binary32 number lies in LDS as its three parts
+    static constexpr int PLANE = XT == DSQ_T_I8 ? 128 : 256;          // bytes of a plane of a block's row in LDS
+    static constexpr int PITCH = PLANES * PLANE + 16;
+    static constexpr int UNITS = PLANE / 16, CH = 128 / UNITS;        // units of a row that a thread stages, channels of one
+    static constexpr int WORDS = CH * ES / 16;                        // 16-byte words of a unit in memory
 };
 
 // Code - zero of a word's eight codes as bytes: 128 + code - zero is between 113 and 143, without carries from byte to byte.
@@ -48,7 +51,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     constexpr int THREADS = 64 * WN * WK, ROWS = 32 * MT, BLOCK = ROWS * L::PITCH;
     constexpr int STEP = WK * BPI;                                    // blocks of an iteration
     constexpr bool DEEP = BPI == 1;                                   // rows are fetched two iterations ahead
-    constexpr int LOADS = ROWS * L::UNITS * STEP / THREADS;             // 16-byte units a thread stages
+    constexpr int LOADS = ROWS * L::UNITS * STEP / THREADS;           // units a thread stages
     constexpr int XSUM = INT ? 0 : GPB * ROWS;                        // sums of x of a block's groups
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][STEP] blocks, then [2][STEP] sums
     float *xsums = reinterpret_cast<float *>(lds + 2 * STEP * BLOCK);
@@ -76,11 +79,14 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
 
     const int unit = threadIdx.x % L::UNITS, line0 = threadIdx.x / L::UNITS;
     constexpr int LINES = THREADS / L::UNITS;                         // rows a load instruction of the workgroup covers
-    v4u xa[LOADS], xb[LOADS];
-    auto load_rows = [&](int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
+    typedef Side<v4u, L::WORDS> Unit;
+    Unit xa[LOADS], xb[LOADS];
+    auto load_rows = [&](int it, Unit (&xr)[LOADS]) __attribute__((always_inline)) {
         if (it >= iters) {                                            // (meets scales of 0: any number will do)
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) xr[j] = (v4u){0u, 0u, 0u, 0u};
+            for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+                for (int k = 0; k < L::WORDS; ++k) xr[j].at[k] = (v4u){0u, 0u, 0u, 0u};
             return;
         }
 #pragma unroll
@@ -88,38 +94,60 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
-            // past the row's end its last 16 bytes: of blocks that meet no weights or scales of 0, or cut off by `cut`
-            const int k = 128 * b + 16 / L::ES * unit, last = (INT ? 128 * KB : a.K) - 16 / L::ES;
-            xr[j] = load_side<v4u, 1>((const v4u *)((const char *)a.x + m * a.x_stride * L::ES + (int64_t)(k < last ? k : last) * L::ES)).at[0];
+            // past the row's end its last unit: of blocks that meet no weights or scales of 0, or cut off by `cut`
+            const int k = 128 * b + L::CH * unit, last = (INT ? 128 * KB : a.K) - L::CH;
+            xr[j] = load_side<v4u, L::WORDS>((const v4u *)((const char *)a.x + (m * a.x_stride + (k < last ? k : last)) * L::ES));
         }
     };
     // Floats of the last block, k..k+7 of a row of K: moved down by as many as lie before k, zeros behind K.
-    auto cut = [&](const v4u &x, int k) __attribute__((always_inline)) {
-        const int back = k + 8 - a.K, n = 16 * (back < 0 ? 0 : back > 8 ? 8 : back);
-        uint64_t at[2];
-        __builtin_memcpy(at, &x, 16);
-        const uint64_t lo = n >= 128 ? 0 : n >= 64 ? at[1] : at[0], hi = n >= 64 ? 0 : at[1];
-        const uint64_t to[2] = {lo >> (n & 63) | hi << 1 << (63 - (n & 63)), hi >> (n & 63)};
-        v4u y;
-        __builtin_memcpy(&y, to, 16);
-        return y;
+    auto cut = [&](Unit &x, int k) __attribute__((always_inline)) {
+        const int back = k + 8 - a.K;
+        if constexpr (XT == DSQ_T_F32) {
+            float at[8];
+            __builtin_memcpy(at, &x, 32);
+#pragma unroll
+            for (int by = 1; by < 8; by *= 2)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) at[i] = back <= 0 || !(back & by) ? at[i] : i + by < 8 ? at[i + by] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) at[i] = back < 8 ? at[i] : 0.0f;
+            __builtin_memcpy(&x, at, 32);
+        } else {
+            const int n = 16 * (back < 0 ? 0 : back > 8 ? 8 : back);
+            uint64_t at[2];
+            __builtin_memcpy(at, &x, 16);
+            const uint64_t lo = n >= 128 ? 0 : n >= 64 ? at[1] : at[0], hi = n >= 64 ? 0 : at[1];
+            const uint64_t to[2] = {lo >> (n & 63) | hi << 1 << (63 - (n & 63)), hi >> (n & 63)};
+            __builtin_memcpy(&x, to, 16);
+        }
     };
     const int it_cut = !INT && a.K % 128 ? iters - 1 : -1;
-    auto store_rows = [&](int to, int it, v4u (&xr)[LOADS]) __attribute__((always_inline)) {
-        if (!INT && it == it_cut)
+    auto store_rows = [&](int to, int it, Unit (&xr)[LOADS]) __attribute__((always_inline)) {
+        if constexpr (!INT)
+            if (it == it_cut)
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) {
-                xr[j] = cut(xr[j], 128 * (it * STEP + (line0 + j * LINES) / ROWS) + 8 * unit);
-                __builtin_amdgcn_sched_barrier(0);                    // (one after the other: side by side they spill)
-            }
+                for (int j = 0; j < LOADS; ++j) {
+                    cut(xr[j], 128 * (it * STEP + (line0 + j * LINES) / ROWS) + 8 * unit);
+                    __builtin_amdgcn_sched_barrier(0);                // (one after the other: side by side they spill)
+                }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int line = line0 + j * LINES, row = line % ROWS, k = line / ROWS;
-            *reinterpret_cast<v4u *>(lds + (to * STEP + k) * BLOCK + row * L::PITCH + 16 * unit) = xr[j];
-            if constexpr (!INT) {
-                // the sum of a group of x: eight channels a lane, 4 * SPG lanes side by side
+            v4u *at = reinterpret_cast<v4u *>(lds + (to * STEP + k) * BLOCK + row * L::PITCH + 16 * unit);
+            if constexpr (INT) {
+                *at = xr[j].at[0];
+            } else {
                 Frag<XT> f;
-                f.v = __builtin_bit_cast(decltype(f.v), xr[j]);
+                __builtin_memcpy(&f, &xr[j], sizeof f);
+                if constexpr (XT == DSQ_T_F32) {
+                    bf16x8 t[3];
+                    split3(f.v, t);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) at[i * L::PLANE / 16] = __builtin_bit_cast(v4u, t[i]);
+                } else {
+                    *at = xr[j].at[0];
+                }
+                // the sum of a group of x: eight channels a lane, 4 * SPG lanes side by side
                 float s = sum8(f);
                 s = lanes_sum<4 * SPG>(s);
                 if (unit % (4 * SPG) == 0) xsums[(to * STEP + k) * XSUM + unit / (4 * SPG) * ROWS + row] = s;
@@ -144,13 +172,13 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     };
     // One block of input channels from LDS block `at`.
     auto block = [&](int at, const v4u (&wv)[2], const uint32_t (&sv)[GPB]) __attribute__((always_inline)) {
-        const char *base = lds + at * BLOCK + r * L::PITCH + 16 * L::ES * h;
+        const char *base = lds + at * BLOCK + r * L::PITCH + (INT ? 16 : 32) * h;
         const float *xsum = xsums + at * XSUM;
         // Units of one group and 32 rows: the matrix instructions of a unit stand beside the scaling of the one before, and its
         // rows are read from LDS one unit ahead.  (Left to itself the compiler reads the rows of all units first and spills, or
         // reads each operand right before its instruction and waits.)
-        constexpr int XF = INT ? SPG : 2 * SPG;           // operands of a unit's rows
-        constexpr int PART = XF < 4 ? XF : 4, PARTS = XF / PART;      // ... of which so many are read ahead
+        constexpr int XF = INT ? SPG : 2 * SPG * L::PLANES;           // operands of a unit's rows
+        constexpr int PART = XF < 4 ? XF : L::PLANES == 3 ? 6 : 4, PARTS = XF / PART;      // ... of which so many are read ahead
         v4i xf[2][PART];
         v16f facc[2];
         v16i iacc[2];
@@ -159,8 +187,8 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             const int g = p / PARTS / MT, i = p / PARTS % MT;
 #pragma unroll
             for (int j = 0; j < PART; ++j) {
-                const int t = p % PARTS * PART + j;
-                xf[p & 1][j] = *reinterpret_cast<const v4i *>(base + 32 * i * L::PITCH + (INT ? 32 * (g * SPG + t) : 64 * (g * SPG + t / 2) + 16 * (t % 2)));
+                const int o = p % PARTS * PART + j, t = o / L::PLANES;
+                xf[p & 1][j] = *reinterpret_cast<const v4i *>(base + 32 * i * L::PITCH + (INT ? 32 * (g * SPG + t) : 64 * (g * SPG + t / 2) + 16 * (t % 2)) + L::PLANE * (o % L::PLANES));
             }
         };
         auto scaled = [&](int u) __attribute__((always_inline)) {
@@ -208,10 +236,10 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 if (p % PARTS) acc = facc[u & 1];
 #pragma unroll
                 for (int j = 0; j < PART; ++j) {
-                    const int t = p % PARTS * PART + j;
+                    const int t = (p % PARTS * PART + j) / L::PLANES;
                     const v4i x = xf[p & 1][j];
                     const uint32_t codes = wv[t % 2][g * SPG + t / 2];
-                    if constexpr (XT == DSQ_T_BF16)
+                    if constexpr (XT != DSQ_T_F16)
                         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), codes_bf16(codes), acc, 0, 0, 0);
                     else
                         acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), codes_f16(codes), acc, 0, 0, 0);
@@ -335,33 +363,41 @@ hipError_t launch_groups(const DsqW4Args &a, hipStream_t stream)
            : a.group == 64 ? launch_of<XT, MT, WN, WK, BPI, 2>(a, stream) : launch_of<XT, MT, WN, WK, BPI, 1>(a, stream);
 }
 
-template <int XT>
-hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
+struct Choice {
+    int rows, channels, time;
+};
+// The choice with the least rounds of its workgroups over the 256 compute units times the time of a round.
+template <int COUNT>
+int least_time(const DsqW4Args &a, const Choice (&of)[COUNT])
 {
-    constexpr bool INT = XT == DSQ_T_I8;
-    // A large tile reads least and unpacks a code for most rows, a small one leaves no compute unit idle: of five tiles the one
-    // with the least rounds over the 256 compute units times its time for a round.  Those times are measured at K = 4096 and
-    // groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
-    //
-    //   rows x N        32x64      64x64      64x128     64x256     128x256
-    //   128 x 4096      13 / 10    20 / 13    25 / 19    37 / 29    63 / 44
-    //   256 x 4096      25 / 13    22 / 14    26 / 20    37 / 29    62 / 44
-    //   512 x 4096      45 / 24    40 / 24    28 / 21    38 / 30    63 / 45
-    //   1024 x 4096    103 / 49    77 / 48    56 / 41    45 / 33    66 / 46
-    //   2048 x 8192    388 / 198  324 / 221  226 / 165  184 / 129  157 / 108
-    struct { int rows, channels, time; } const tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 13 : 20}, {64, 128, INT ? 20 : 27},
-                                                           {64, 256, INT ? 30 : 41}, {128, 256, INT ? 48 : 76}};
     int best = 0;
     int64_t least = INT64_MAX;
-    for (int i = 0; i < 5; ++i) {
-        const int64_t count = (((int64_t)a.M + tiles[i].rows - 1) / tiles[i].rows) * (((int64_t)a.N + tiles[i].channels - 1) / tiles[i].channels);
-        const int64_t time = (count + 255) / 256 * tiles[i].time;
+    for (int i = 0; i < COUNT; ++i) {
+        const int64_t count = (((int64_t)a.M + of[i].rows - 1) / of[i].rows) * (((int64_t)a.N + of[i].channels - 1) / of[i].channels);
+        const int64_t time = (count + 255) / 256 * of[i].time;
         if (time < least) {
             least = time;
             best = i;
         }
     }
-    switch (best) {
+    return best;
+}
+
+// A large tile reads least and unpacks a code for most rows, a small one leaves no compute unit idle.  The times of a round are
+// measured at K = 4096 and groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
+//
+//   rows x N        32x64      64x64      64x128     64x256     128x256
+//   128 x 4096      13 / 10    20 / 13    25 / 19    37 / 29    63 / 44
+//   256 x 4096      25 / 13    22 / 14    26 / 20    37 / 29    62 / 44
+//   512 x 4096      45 / 24    40 / 24    28 / 21    38 / 30    63 / 45
+//   1024 x 4096    103 / 49    77 / 48    56 / 41    45 / 33    66 / 46
+//   2048 x 8192    388 / 198  324 / 221  226 / 165  184 / 129  157 / 108
+template <int XT>
+hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
+{
+    constexpr bool INT = XT == DSQ_T_I8;
+    const Choice tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 13 : 20}, {64, 128, INT ? 20 : 27}, {64, 256, INT ? 30 : 41}, {128, 256, INT ? 48 : 76}};
+    switch (least_time(a, tiles)) {
     case 0: return launch_groups<XT, 1, 2, 4>(a, stream);
     case 1: return launch_groups<XT, 2, 2, 4>(a, stream);
     case 2: return launch_groups<XT, 2, 4, 2>(a, stream);
@@ -370,10 +406,32 @@ hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
     }
 }
 
+// Binary32 rows take three times the LDS and matrix instructions, and the kernel for a few rows is one of the choices:
+//
+//   rows x N       16x16 (w4_rows)   32x128   32x256   64x256
+//   16 x 4096      13
+//   64 x 4096      37                32       46       78
+//   512 x 4096     240               75       62       80
+//   1024 x 4096    480               146      117      103
+hipError_t launch_f32(const DsqW4Args &a, hipStream_t stream)
+{
+    const Choice tiles[4] = {{16, 16, 9}, {32, 128, 33}, {32, 256, 58}, {64, 256, 100}};
+    switch (a.K < 8 ? 0 : least_time(a, tiles)) {                     // (the tiles take eight channels of a row at a time)
+    case 0: return dsq_launch_w4_rows(a, stream);
+    case 1: return launch_groups<DSQ_T_F32, 1, 4, 2>(a, stream);
+    case 2: return launch_groups<DSQ_T_F32, 1, 8, 1>(a, stream);
+    default: return launch_groups<DSQ_T_F32, 2, 8, 1>(a, stream);
+    }
+}
+
 }  // namespace
 
-hipError_t dsq_launch_w4_tiles(const DsqW4Args &a, hipStream_t stream)
+hipError_t dsq_launch_w4_linear(const DsqW4Args &a, hipStream_t stream)
 {
-    return a.x_type == DSQ_T_I8 ? launch_tiles<DSQ_T_I8>(a, stream)
-           : a.x_type == DSQ_T_F16 ? launch_tiles<DSQ_T_F16>(a, stream) : launch_tiles<DSQ_T_BF16>(a, stream);
+    if (a.M == 1) return dsq_launch_w4_row(a, stream);
+    if (a.x_type == DSQ_T_F32) return launch_f32(a, stream);
+    if (a.x_type == DSQ_T_I8) return a.M <= 16 ? dsq_launch_w4_rows(a, stream) : launch_tiles<DSQ_T_I8>(a, stream);
+    // (as above: the tiles take eight channels of a row at a time)
+    if (a.M <= 16 || a.K < 8) return dsq_launch_w4_rows(a, stream);
+    return a.x_type == DSQ_T_F16 ? launch_tiles<DSQ_T_F16>(a, stream) : launch_tiles<DSQ_T_BF16>(a, stream);
 }
