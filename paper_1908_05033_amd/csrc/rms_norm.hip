@@ -91,9 +91,10 @@ __device__ __forceinline__ Raw<E> in_row(Raw<E> r, int at, int dim)
         if (back > 0) r.lo = r.hi = 0;
     } else if (dim >= V) {
         const int n = 8 * (int)sizeof(E) * (back < 0 ? 0 : back < V ? back : V);
-        const uint64_t lo = r.lo, hi = r.hi;
-        r.lo = n == 0 ? lo : n < 64 ? lo >> n | hi << (64 - n) : n < 128 ? hi >> (n - 64) : 0;
-        r.hi = n < 64 ? hi >> n : 0;
+        // (without branches: 0, 64 and 128 are moves of whole halves)
+        const uint64_t lo = n >= 128 ? 0 : n >= 64 ? r.hi : r.lo, hi = n >= 64 ? 0 : r.hi;
+        r.lo = lo >> (n & 63) | hi << 1 << (63 - (n & 63));
+        r.hi = hi >> (n & 63);
     }
     return r;
 }
@@ -118,6 +119,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_kernel(DsqN
     constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR, WAVES = THREADS / 64;
     __shared__ double part[2][2][WAVES];      // (rows of more than a wave)
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    if (VPT > 1) __builtin_assume(a.dim > TPR * V);
     float w[N];
     float mark = 0.0f;       // NaN once a weight is not finite
 #pragma unroll
@@ -149,12 +151,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_kernel(DsqN
         const int64_t row = base + sub;
         const bool live = row < a.rows;
         if (!AHEAD) load(row);
+        int dim = a.dim;
+        asm volatile("" : "+s"(dim));                           // (which elements exist is found again for each row: kept, the answers spill)
+        if (VPT > 1) __builtin_assume(dim > TPR * V);
         float h[N];
         double ss = 0.0, amax = 0.0;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int at = (t + j * TPR) * V;
-            const Raw<E> x = in_row<E, V, WHOLE>(xv[j], at, a.dim), res = in_row<E, V, WHOLE>(rv[j], at, a.dim);
+            const Raw<E> x = in_row<E, V, WHOLE>(xv[j], at, dim), res = in_row<E, V, WHOLE>(rv[j], at, dim);
             Side<E, V> sv;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -165,7 +170,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_kernel(DsqN
                 ss = __builtin_fma((double)f, (double)f, ss);
                 amax = fmax(amax, fabs((double)f * (double)w[j * V + v]));
             }
-            if (a.sum && live) store_in_row<E, V, WHOLE>((E *)a.sum + row * a.dim, at, a.dim, sv);
+            if (a.sum && live) store_in_row<E, V, WHOLE>((E *)a.sum + row * a.dim, at, dim, sv);
         }
         if (AHEAD) load(row + (int64_t)gridDim.x * RPB);
         if (mark != 0.0f) amax = __builtin_inf();
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_kernel(DsqN
                 Side<E, V> yv;
 #pragma unroll
                 for (int v = 0; v < V; ++v) yv.at[v] = (E)(float)((double)h[j * V + v] * (double)w[j * V + v] * r);
-                store_in_row<E, V, WHOLE>((E *)a.y + row * a.dim, at, a.dim, yv);
+                store_in_row<E, V, WHOLE>((E *)a.y + row * a.dim, at, dim, yv);
             }
         if (a.codes) {
             const float inv32 = (float)inv;
@@ -293,6 +298,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_bwd_kernel(
     __shared__ float part[2][WAVES];
     __shared__ float rows_gw[RPB > 1 ? TPR * VPT * V : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    if (VPT > 1) __builtin_assume(a.dim > TPR * V);
     float *partial = gridDim.x == 1 ? a.grad_weight : a.partial + (size_t)blockIdx.x * a.dim;
     float w[VPT * V], gw[VPT * V];
 #pragma unroll
@@ -321,24 +327,29 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_bwd_kernel(
         const int64_t row = base + sub;
         const bool live = row < a.rows;
         if (!AHEAD) load(row);
+        int dim = a.dim;
+        asm volatile("" : "+s"(dim));                           // (as in the forward pass)
+        if (VPT > 1) __builtin_assume(dim > TPR * V);
         const float r = live ? rs : 0.0f;
-        float n[VPT * V], gw_of[VPT * V], s[VPT * V];
+        float n[VPT * V], gw_of[VPT * V];
         float along = 0.0f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int at = (t + j * TPR) * V;
-            const Raw<E> hr = in_row<E, V, WHOLE>(hv[j], at, a.dim), gr = in_row<E, V, WHOLE>(gv[j], at, a.dim), sr = in_row<E, V, WHOLE>(sv[j], at, a.dim);
+            const Raw<E> hr = in_row<E, V, WHOLE>(hv[j], at, dim), gr = in_row<E, V, WHOLE>(gv[j], at, dim);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int i = j * V + v;
                 const float g = live ? gr[v] : 0.0f;
                 n[i] = live ? hr[v] * r : 0.0f;
-                s[i] = sr[v];
                 gw[i] = __builtin_fmaf(g, n[i], gw[i]);
                 gw_of[i] = g * w[i];
                 along = __builtin_fmaf(gw_of[i], n[i], along);
             }
         }
+        Raw<E> sw[VPT];
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) sw[j] = sv[j];
         if (AHEAD) load(row + (int64_t)gridDim.x * RPB);
         along = lane_sum(along, TPR < 64 ? TPR : 64);
         if (TPR > 64) {
@@ -355,11 +366,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_norm_bwd_kernel(
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int at = (t + j * TPR) * V;
+            const Raw<E> s = in_row<E, V, WHOLE>(sw[j], at, dim);
             Side<E, V> ov;
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                ov.at[v] = (E)__builtin_fmaf(r, __builtin_fmaf(-n[j * V + v], along, gw_of[j * V + v]), s[j * V + v]);
-            store_in_row<E, V, WHOLE>((E *)a.grad_x + row * a.dim, at, a.dim, ov);
+                ov.at[v] = (E)__builtin_fmaf(r, __builtin_fmaf(-n[j * V + v], along, gw_of[j * V + v]), s[v]);
+            store_in_row<E, V, WHOLE>((E *)a.grad_x + row * a.dim, at, dim, ov);
         }
     }
     if (!a.grad_weight) return;
