@@ -10,10 +10,11 @@
 // vector instructions an element, which no matrix instruction can take over).  Floats: the operand is the code, and the group's
 // sum of x, from the staging of the rows, carries the zero point.
 //
-// Measured at K = 4096 and groups of 128: 2048 rows to 8192 channels 107 us (1.28 POP/s) with 8-bit rows, 158 us (0.87
-// PFLOP/s) with bfloat16 ones, bound by the matrix instructions' issue between barriers and the scaling beside it.  256 rows to 4096: 14
-// and 22 us.  Of the latter a call without work is 6, and for its 16 million codes the loads alone, the writes to LDS alone and the
-// multiplication alone would take 8, 4 and 10: they overlap in part only, with one workgroup on a compute unit.
+// Measured at K = 4096 and groups of 128: 2048 rows to 8192 channels 99 us (1.39 POP/s) with 8-bit rows, 156 us (0.88 PFLOP/s)
+// with bfloat16 ones.  Of the former the vector instructions (15 for a matrix instruction: the scaling of the groups 8, the
+// unpacking 4) fill 60 and the matrix instructions 30 of a compute unit's time; with two waves on a SIMD they overlap in part.
+// 256 rows to 4096: 12 and 21 us.  Of the latter a call without work is 6, and for its 16 million codes the loads alone, the writes to
+// LDS alone and the multiplication alone would take 8, 4 and 10: with one workgroup on a compute unit they too overlap in part.
 #include <type_traits>
 
 #include "w4_device.h"
@@ -82,7 +83,9 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     typedef Side<v4u, L::WORDS> Unit;
     Unit xa[LOADS], xb[LOADS];
     auto load_rows = [&](int it, Unit (&xr)[LOADS]) __attribute__((always_inline)) {
-        if (it >= iters) {                                            // (meets scales of 0: any number will do)
+        // (8-bit rows without a branch around the loads: where it next waits for a scale the compiler would wait for them too, 107 us
+        // for 98 at 2048 x 4096 to 8192.  Floats win nothing by it, and lose what the loads past the end take.)
+        if (!INT && it >= iters) {                                    // (meets scales of 0: any number will do)
 #pragma unroll
             for (int j = 0; j < LOADS; ++j)
 #pragma unroll
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
-            // past the row's end its last unit: of blocks that meet no weights or scales of 0, or cut off by `cut`
+            // past the row's end its last unit: of blocks that meet no weights or scales of 0, or cut off by `cut`.
             const int k = 128 * b + L::CH * unit, last = (INT ? 128 * KB : a.K) - L::CH;
             xr[j] = load_side<v4u, L::WORDS>((const v4u *)((const char *)a.x + (m * a.x_stride + (k < last ? k : last)) * L::ES));
         }
@@ -247,6 +250,12 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 facc[u & 1] = acc;
             }
             if (u > 0 && p % PARTS == 0) scaled(u - 1);
+            if constexpr (INT)                                        // (a share of the scaling behind each matrix instruction)
+#pragma unroll
+                for (int t = 0; t < SPG; ++t) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 32 / SPG, 0);
+                }
             __builtin_amdgcn_sched_barrier(0);
         }
         scaled(GPB * MT - 1);
