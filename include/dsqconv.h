@@ -463,7 +463,7 @@ dsq_status dsq_rms_norm_bwd(const void *h, int64_t h_stride, const void *weight,
  * With w alone each group gets, in binary32, the range from min(w, 0) to max(w, 0):
  *     scale = (max - min) / 15, kept to 20 bits;  zero = rint(-min / scale)
  * and with w in any case  code = clamp(rint(w / scale) + zero, 0, 15); a scale of 0 has
- * code = zero.
+ * code = zero.  Weights and scales are finite numbers.
  */
 dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
                                const float *scale, const uint8_t *zero, int N, int K,
@@ -479,7 +479,7 @@ dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
  * x          device, [M] rows of K elements of dtype
  * bias       device, [N] of dtype, or NULL
  * out        device, out, [M] rows of N elements of dtype, out_stride >= N elements from row
- *            to row; what lies between them is left as it is
+ *            to row; what lies between them is left as it is; overlaps no input
  */
 dsq_status dsq_linear_w4(const void *x, int64_t x_stride, dsq_dtype dtype, int M,
                          int N, int K, int group, const void *w_packed,
