@@ -82,18 +82,23 @@ __device__ __forceinline__ long codes_i8(uint32_t w)
     return (long)(lo | hi << 32);
 }
 
-// x = t[0] + t[1] + t[2] exactly, eight significant bits each (an infinity or NaN is t[0] alone).
+// x = t[0] + t[1] + t[2] exactly, eight significant bits each, cut towards zero: the upper halves of x and of what remains, two
+// numbers moved at a time.  (An infinity or a NaN leaves NaN in t[1] and t[2], and makes its row NaN.)
 __device__ __forceinline__ void split3(const float (&x)[8], bf16x8 (&t)[3])
 {
+    uint32_t to[3][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = __uint_as_float(__float_as_uint(x[i]) & 0xFFFF0000u);
-        const float r = __builtin_isinf(x[i]) ? 0.0f : x[i] - a;
-        const float b = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
-        t[0][i] = (__bf16)a;
-        t[1][i] = (__bf16)b;
-        t[2][i] = (__bf16)(r - b);
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            to[k][i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+            a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+            b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+        }
     }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) __builtin_memcpy(&t[k], to[k], 16);
 }
 
 // The sum over 4, 8 or 16 lanes side by side, in each of them: lanes exchanged by one and by two, then halves and rows of 16 mirrored.
