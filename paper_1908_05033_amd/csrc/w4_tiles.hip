@@ -396,16 +396,16 @@ int least_time(const DsqW4Args &a, const Choice (&of)[COUNT])
 // measured at K = 4096 and groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
 //
 //   rows x N        32x64      64x64      64x128     64x256     128x256
-//   128 x 4096      13 / 10    20 / 13    25 / 19    37 / 29    63 / 44
-//   256 x 4096      25 / 13    22 / 14    26 / 20    37 / 29    62 / 44
-//   512 x 4096      45 / 24    40 / 24    28 / 21    38 / 30    63 / 45
-//   1024 x 4096    103 / 49    77 / 48    56 / 41    45 / 33    66 / 46
-//   2048 x 8192    388 / 198  324 / 221  226 / 165  184 / 129  157 / 108
+//   128 x 4096      14 / 9     20 / 12    25 / 17    37 / 26    63 / 40
+//   256 x 4096      25 / 13    21 / 12    26 / 17    37 / 27    62 / 40
+//   512 x 4096      48 / 23    41 / 23    30 / 18    39 / 27    63 / 41
+//   1024 x 4096    103 / 47    80 / 46    59 / 37    47 / 32    67 / 42
+//   2048 x 8192    388 / 185  325 / 200  225 / 146  179 / 121  158 / 101
 template <int XT>
 hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 {
     constexpr bool INT = XT == DSQ_T_I8;
-    const Choice tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 13 : 20}, {64, 128, INT ? 20 : 27}, {64, 256, INT ? 30 : 41}, {128, 256, INT ? 48 : 76}};
+    const Choice tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 12 : 20}, {64, 128, INT ? 18 : 27}, {64, 256, INT ? 28 : 41}, {128, 256, INT ? 46 : 76}};
     switch (least_time(a, tiles)) {
     case 0: return launch_groups<XT, 1, 2, 4>(a, stream);
     case 1: return launch_groups<XT, 2, 2, 4>(a, stream);
@@ -418,10 +418,10 @@ hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 // Binary32 rows take three times the LDS and matrix instructions, and the kernel for a few rows is one of the choices:
 //
 //   rows x N       16x16 (w4_rows)   32x128   32x256   64x256
-//   16 x 4096      13
-//   64 x 4096      37                32       46       78
-//   512 x 4096     240               75       62       80
-//   1024 x 4096    480               146      117      103
+//   16 x 4096      12                29       45       77
+//   64 x 4096      35                30       45       78
+//   512 x 4096     236               71       61       83
+//   1024 x 4096    468               139      112      101
 hipError_t launch_f32(const DsqW4Args &a, hipStream_t stream)
 {
     const Choice tiles[4] = {{16, 16, 9}, {32, 128, 33}, {32, 256, 58}, {64, 256, 100}};
