@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "w4_device.h"
+#include "w4_plan.h"
 
 namespace {
 
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     const int KB = dsq_w4_round(a.K) / 128, Gp = KB * GPB, iters = (KB + STEP - 1) / STEP;
     const int n0 = nt * 32 * WN + 32 * wn;
     // this lane's channel: 16-channel block (r / 16), column r % 16; its halves of 16 input channels
-    const size_t ct = (size_t)(n0 / 16 + r / 16);
+    const size_t ct = (size_t)w4_channel_tile(a.N, n0, r);
     const v4u *w = reinterpret_cast<const v4u *>(a.w) + ct * KB * 64 + 32 * h + r % 16;
     const uint32_t *sc = a.scales + ct * Gp * 16 + r % 16;
 
@@ -372,41 +373,11 @@ hipError_t launch_groups(const DsqW4Args &a, hipStream_t stream)
            : a.group == 64 ? launch_of<XT, MT, WN, WK, BPI, 2>(a, stream) : launch_of<XT, MT, WN, WK, BPI, 1>(a, stream);
 }
 
-struct Choice {
-    int rows, channels, time;
-};
-// The choice with the least rounds of its workgroups over the 256 compute units times the time of a round.
-template <int COUNT>
-int least_time(const DsqW4Args &a, const Choice (&of)[COUNT])
-{
-    int best = 0;
-    int64_t least = INT64_MAX;
-    for (int i = 0; i < COUNT; ++i) {
-        const int64_t count = (((int64_t)a.M + of[i].rows - 1) / of[i].rows) * (((int64_t)a.N + of[i].channels - 1) / of[i].channels);
-        const int64_t time = (count + 255) / 256 * of[i].time;
-        if (time < least) {
-            least = time;
-            best = i;
-        }
-    }
-    return best;
-}
-
-// A large tile reads least and unpacks a code for most rows, a small one leaves no compute unit idle.  The times of a round are
-// measured at K = 4096 and groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
-//
-//   rows x N        32x64      64x64      64x128     64x256     128x256
-//   128 x 4096      14 / 9     20 / 12    25 / 17    37 / 26    63 / 40
-//   256 x 4096      25 / 13    21 / 12    26 / 17    37 / 27    62 / 40
-//   512 x 4096      48 / 23    41 / 23    30 / 18    39 / 27    63 / 41
-//   1024 x 4096    103 / 47    80 / 46    59 / 37    47 / 32    67 / 42
-//   2048 x 8192    388 / 185  325 / 200  225 / 146  179 / 121  158 / 101
 template <int XT>
 hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
 {
     constexpr bool INT = XT == DSQ_T_I8;
-    const Choice tiles[5] = {{32, 64, INT ? 8 : 13}, {64, 64, INT ? 12 : 20}, {64, 128, INT ? 18 : 27}, {64, 256, INT ? 28 : 41}, {128, 256, INT ? 46 : 76}};
-    switch (least_time(a, tiles)) {
+    switch (w4_least_time(a.M, a.N, INT ? kW4Codes : kW4Half)) {
     case 0: return launch_groups<XT, 1, 2, 4>(a, stream);
     case 1: return launch_groups<XT, 2, 2, 4>(a, stream);
     case 2: return launch_groups<XT, 2, 4, 2>(a, stream);
@@ -415,17 +386,9 @@ hipError_t launch_tiles(const DsqW4Args &a, hipStream_t stream)
     }
 }
 
-// Binary32 rows take three times the LDS and matrix instructions, and the kernel for a few rows is one of the choices:
-//
-//   rows x N       16x16 (w4_rows)   32x128   32x256   64x256
-//   16 x 4096      12                29       45       77
-//   64 x 4096      35                30       45       78
-//   512 x 4096     236               71       61       83
-//   1024 x 4096    468               139      112      101
 hipError_t launch_f32(const DsqW4Args &a, hipStream_t stream)
 {
-    const Choice tiles[4] = {{16, 16, 9}, {32, 128, 33}, {32, 256, 58}, {64, 256, 100}};
-    switch (a.K < 8 ? 0 : least_time(a, tiles)) {                     // (the tiles take eight channels of a row at a time)
+    switch (a.K < 8 ? 0 : w4_least_time(a.M, a.N, kW4Single)) {       // (the tiles take eight channels of a row at a time)
     case 0: return dsq_launch_w4_rows(a, stream);
     case 1: return launch_groups<DSQ_T_F32, 1, 4, 2>(a, stream);
     case 2: return launch_groups<DSQ_T_F32, 1, 8, 1>(a, stream);
