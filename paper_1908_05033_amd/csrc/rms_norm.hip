@@ -6,7 +6,7 @@
 // r cancels in a code, so sum of squares and amax come out of one pass over registers and a code is decided by h and
 // w alone.  Squares, products and the quotient are formed in binary64, in which the product of two binary32 numbers is
 // exact: nothing over- or underflows over the whole range of the types, y is rounded once, and a code is the
-// correctly rounded quotient.
+// correctly rounded quotient (one beside a half is decided exactly, code_of).
 //
 //   backward, t = gy * w, n = h * r:  gx = r * (t - n * mean(t * n)) + gsum,  gw = sum over rows of gy * n
 //
@@ -34,13 +34,21 @@ __device__ __forceinline__ double lane_max(double v, int lanes)
     return v;
 }
 
-// The code of the product p: its quotient by the step amax / 127, rounded to the nearest integer.  p * inv is within
-// 2^-44 of the quotient; only one that near to a half is divided out.
+// The code of the product p: its quotient by the step amax / 127, rounded to the nearest integer, halves to even.  p * inv is within
+// 2^-44 of the quotient; one that near to a half, whole + 1/2, is decided by the sign of 254 |p| - (2 whole + 1) amax.  p and amax
+// have 48 significant bits, so a factor of 8 bits leaves each product a few bits longer than a binary64 number: both are taken with
+// what their rounding left, and their difference is exact.
 __device__ __forceinline__ int code_of(double p, double inv, double amax)
 {
     const double t = p * inv;
     const double n = rint(t);
-    if (__builtin_expect(fabs(t - n) > 0.5 - 0x1p-40, 0)) return (int)rint(127.0 * p / amax);
+    if (__builtin_expect(fabs(t - n) > 0.5 - 0x1p-40, 0)) {
+        const double whole = floor(fabs(t)), odd = 2.0 * whole + 1.0, size = fabs(p);
+        const double a = 254.0 * size, b = odd * amax;
+        const double past = (a - b) + (__builtin_fma(254.0, size, -a) - __builtin_fma(odd, amax, -b));
+        const int code = (int)whole, up = past > 0.0 || (past == 0.0 && (code & 1));
+        return p < 0.0 ? -(code + up) : code + up;
+    }
     return (int)n;
 }
 
