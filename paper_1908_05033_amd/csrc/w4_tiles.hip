@@ -98,12 +98,12 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
-            // past the row's end its last unit: of blocks that meet no weights or scales of 0, or cut off by `cut`.
+            // past the row's end its last unit: of blocks that meet scales of 0 (8-bit rows), or cut off by `cut`.
             const int k = 128 * b + L::CH * unit, last = (INT ? 128 * KB : a.K) - L::CH;
             xr[j] = load_side<v4u, L::WORDS>((const v4u *)((const char *)a.x + (m * a.x_stride + (k < last ? k : last)) * L::ES));
         }
     };
-    // Floats of the last block, k..k+7 of a row of K: moved down by as many as lie before k, zeros behind K.
+    // Floats of the last blocks, k..k+7 of a row of K: moved down by as many as lie before k, zeros behind K.
     auto cut = [&](Unit &x, int k) __attribute__((always_inline)) {
         const int back = k + 8 - a.K;
         if constexpr (XT == DSQ_T_F32) {
@@ -125,7 +125,9 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             __builtin_memcpy(&x, to, 16);
         }
     };
-    const int it_cut = !INT && a.K % 128 ? iters - 1 : -1;
+    // (the last iteration's blocks past the row's end are zeros too: they meet scales of 0, under which a sum of finite numbers
+    // that overflows would be a NaN)
+    const int it_cut = !INT && a.K % (128 * STEP) ? iters - 1 : -1;
     auto store_rows = [&](int to, int it, Unit (&xr)[LOADS]) __attribute__((always_inline)) {
         if constexpr (!INT)
             if (it == it_cut)
