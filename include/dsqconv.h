@@ -475,7 +475,9 @@ dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
  *                 scale[n][g] * sum over k in g of (code[n][k] - zero[n][g]) * x[m][k]
  * Codes and activations enter the matrix instruction exactly (a float32 activation in three
  * parts), sums are binary32, and the result is rounded to dtype once.  The zero point's
- * share is formed from the group's sum of x, so sums reach 15 times that of |x|.
+ * share is formed from the group's sum of x, so sums reach 15 times that of |x|.  A result
+ * whose sums pass the range of binary32 on the way is formed again in binary64: rows of
+ * finite numbers give what the formula does, some hundred times slower from about 1e34 on.
  * x          device, [M] rows of K elements of dtype
  * bias       device, [N] of dtype, or NULL
  * out        device, out, [M] rows of N elements of dtype, out_stride >= N elements from row

@@ -148,6 +148,8 @@ __global__ __launch_bounds__(64 * WAVES) void w4_row_kernel(DsqW4Args a, int KS,
     }
     const int n = 16 * nt + r;
     if (mine >= tiles || n >= a.N || lane >= 16) return;
+    if constexpr (kSumsOverflow<XT>)
+        if (__builtin_expect(overflowed(sum), 0)) sum = product_in_64_bits<XT>(0, n);
     if (XT == DSQ_T_I8) sum *= a.x_scale[0];
     if (a.bias) sum += load_out(a.bias, n, a.out_type);
     store_out(a.out, n, a.out_type, sum);

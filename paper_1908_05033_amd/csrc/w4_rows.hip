@@ -160,14 +160,23 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(DsqW4Args a)
         const int n = 16 * ((int)blockIdx.x * NT + i) + r;
         if (n >= a.N) continue;
         const float bias = a.bias ? load_out(a.bias, n, a.out_type) : 0.0f;
+        uint32_t again = 0;                         // results to be formed again
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t m = m0 + 4 * q + c;
             if (m >= a.M) continue;
+            if (kSumsOverflow<XT>) again |= overflowed(v[c]) ? 1u << c : 0u;
             float o = XT == DSQ_T_I8 ? v[c] * a.x_scale[m] : v[c];
             if (a.bias) o += bias;
             store_out(a.out, m * a.out_stride + n, a.out_type, o);
         }
+        if constexpr (kSumsOverflow<XT>)
+            for (; again; again &= again - 1) {
+                const int64_t m = m0 + 4 * q + __builtin_ctz(again);
+                float o = product_in_64_bits<XT>(m, n);
+                if (a.bias) o += bias;
+                store_out(a.out, m * a.out_stride + n, a.out_type, o);
+            }
     }
 }
 

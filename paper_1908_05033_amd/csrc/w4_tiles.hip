@@ -311,11 +311,12 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
     auto store = [&](auto type) __attribute__((always_inline)) {
         typedef decltype(type) E;
         const float bias = a.bias ? (float)((const E *)a.bias)[n] : 0.0f;
+        float mark = 0.0f;                                            // NaN once a sum has overflowed
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = m0 + 32 * i + 8 * wk + 4 * h;           // the lane's first row of the tile
             const int live = a.M - m < 32 ? (int)(a.M - m) : 32;
-            if (live <= 0) return;
+            if (live <= 0) break;
             float scale[4 * QS];
             if constexpr (INT)
 #pragma unroll
@@ -339,10 +340,22 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 for (int c = 0; c < 4; ++c) {
                     float o = INT ? s[c] * scale[4 * j + c] : s[c];
                     if (a.bias) o += bias;
+                    if (kSumsOverflow<XT>) mark = __builtin_fmaf(s[c], 0.0f, mark);
                     if (8 * WK * j + c < live) out[(8 * WK * j + c) * a.out_stride] = (E)o;
                 }
             }
         }
+        if constexpr (kSumsOverflow<XT>)
+            if (__builtin_expect(mark != 0.0f, 0))                    // (the lane looks through what it has stored)
+                for (int e = 0; e < 4 * QS * MT; ++e) {
+                    const int64_t m = m0 + 32 * (e / (4 * QS)) + 8 * wk + 4 * h + 8 * WK * (e / 4 % QS) + e % 4;
+                    if (m >= a.M) break;
+                    E *out = (E *)a.out + m * a.out_stride + n;
+                    if (!overflowed((float)*out)) continue;
+                    float o = product_in_64_bits<XT>(m, n);
+                    if (a.bias) o += bias;
+                    *out = (E)o;
+                }
     };
     if constexpr (!INT) store((typename Element<INT ? DSQ_T_F32 : XT>::type)0.0f);
     else if (a.out_type == DSQ_T_BF16) store((__bf16)0.0f);

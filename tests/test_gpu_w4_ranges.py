@@ -2,16 +2,19 @@
 
 Tolerances as derived in test_gpu_w4.py: they are relative to the sum A of |scale| (code + zero) |x| and to the result, and hold
 wherever the result lies in the type's range, however large or small the sums of codes times x are on the way."""
+import numpy as np
 import pytest
 import torch
 
-from lm_helpers import host, normal, pack, random_w4
+from lm_helpers import DTYPES, host, normal, pack, random_w4
 from test_gpu_w4 import check, run_w4
 
 pytestmark = pytest.mark.gpu
 
 # rows and channels that take one row's kernel, the one of a few rows, and each tile
 SHAPES = [(1, 40), (1, 9000), (5, 40), (16, 9230), (40, 48), (40, 4093), (256, 4093), (512, 4093), (900, 4093), (1024, 4224)]
+# ... and the tiles of binary32 rows
+SHAPES_F32 = [(1, 40), (1, 9000), (5, 40), (64, 4093), (2048, 640), (300, 12400)]
 
 
 def check_some(out, x, c, s, z, group, bias=None):
@@ -32,3 +35,58 @@ def test_large_numbers_at_the_end_of_a_row(M, N, K):
     assert 15 * 8 * float(x.abs().max()) < 2.0 ** 127
     for dt in (torch.bfloat16, torch.float32):
         check_some(run_w4(x.to(dt), p, N, K, group), x.to(dt), c, s, z, group)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,group", [(300, 64), (1024, 128), (100, 32), (7, 32)])
+def test_sums_of_codes_past_the_range(dtype, K, group):
+    """Rows whose products with the codes pass 2^128 though the result does not."""
+    dt = DTYPES[dtype]
+    for M, N in SHAPES_F32 if dtype == "f32" else SHAPES:
+        c, s, z = random_w4(M, N, K, group)
+        s *= np.float32(2.0 ** -10)
+        p = pack(c, s, z, group)
+        for f in (1e28, 1e31, 1e34, 1e36, 5e37):
+            x = normal(M, M, K).clamp(-5, 5).mul(f).to(dt)
+            x[::3, :] = normal(M, M, K, dtype=dt)[::3]
+            assert torch.isfinite(x).all()
+            bias = normal(2, N, dtype=dt)
+            check_some(run_w4(x, p, N, K, group, bias), x, c, s, z, group, bias)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_numbers_with_other_signs_and_a_result_past_the_range(dtype):
+    """A result past the type's largest number is infinite, with its sign, and no other result is."""
+    dt, K, group = DTYPES[dtype], 256, 64
+    for M, N in SHAPES_F32 if dtype == "f32" else SHAPES:
+        c, s, z = random_w4(M, N, K, group)
+        c[:], z[:] = 15, 0
+        s[:] = 2.0 ** -6
+        s[1::2] = -2.0 ** -6
+        s[2::4] = 2.0 ** -20
+        p = pack(c, s, z, group)
+        x = torch.full((M, K), 3e37, dtype=dt, device="cuda")
+        out = run_w4(x, p, N, K, group)
+        want = torch.full((N,), float("inf"), device="cuda")
+        want[1::2] *= -1
+        level = torch.arange(N, device="cuda") % 4 == 2
+        assert torch.equal(out.float()[:, ~level], want[~level].expand(M, -1))
+        assert torch.isfinite(out[:, level]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_that_are_not_finite_beside_large_ones(dtype):
+    dt, K, group = DTYPES[dtype], 300, 64
+    big = 3e4 if dtype == "f16" else 1e37
+    for M, N in SHAPES_F32 if dtype == "f32" else SHAPES:
+        if M < 4:
+            continue
+        c, s, z = random_w4(M, N, K, group)
+        s *= np.float32(2.0 ** -10)
+        p = pack(c, s, z, group)
+        x = normal(M, M, K).clamp(-2, 2).mul(big).to(dt)
+        x[1, 5], x[2, 299], x[3] = float("nan"), float("inf"), float("-inf")
+        out = run_w4(x, p, N, K, group)
+        assert torch.isnan(out[1]).all() and not torch.isfinite(out[2]).any() and not torch.isfinite(out[3]).any()
+        keep = [i for i in range(M) if i not in (1, 2, 3)]
+        check_some(out[keep], x[keep], c, s, z, group)
