@@ -95,10 +95,12 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
         }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int line = line0 + j * LINES, row = line % ROWS, b = it * STEP + line / ROWS;
+            const int line = line0 + j * LINES, row = line % ROWS, at = it * STEP + line / ROWS;
             int64_t m = m0 + row;
             m = m < a.M ? m : a.M - 1;                                // (past the end: loaded and not stored)
-            // past the row's end its last unit: of blocks that meet scales of 0 (8-bit rows), or cut off by `cut`.
+            // past the last block floats of that one again, as its weights: what overflows under scales of 0 has done so before.  Past
+            // the row's end its last unit: of levels or scales of 0 (8-bit rows), or cut off by `cut`.
+            const int b = INT ? at : min(at, KB - 1);
             const int k = 128 * b + L::CH * unit, last = (INT ? 128 * KB : a.K) - L::CH;
             xr[j] = load_side<v4u, L::WORDS>((const v4u *)((const char *)a.x + (m * a.x_stride + (k < last ? k : last)) * L::ES));
         }
@@ -125,9 +127,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             __builtin_memcpy(&x, to, 16);
         }
     };
-    // (the last iteration's blocks past the row's end are zeros too: they meet scales of 0, under which a sum of finite numbers
-    // that overflows would be a NaN)
-    const int it_cut = !INT && a.K % (128 * STEP) ? iters - 1 : -1;
+    const int it_cut = !INT && a.K % 128 ? iters - 1 : -1;
     auto store_rows = [&](int to, int it, Unit (&xr)[LOADS]) __attribute__((always_inline)) {
         if constexpr (!INT)
             if (it == it_cut)
