@@ -477,7 +477,8 @@ dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
  * parts), sums are binary32, and the result is rounded to dtype once.  The zero point's
  * share is formed from the group's sum of x, so sums reach 15 times that of |x|.  A result
  * whose sums pass the range of binary32 on the way is formed again in binary64: rows of
- * finite numbers give what the formula does, some hundred times slower from about 1e34 on.
+ * finite numbers give what the formula does, some hundred times slower from about 1e34
+ * (bfloat16) and 1e28 (float32) on.
  * x          device, [M] rows of K elements of dtype
  * bias       device, [N] of dtype, or NULL
  * out        device, out, [M] rows of N elements of dtype, out_stride >= N elements from row

@@ -105,6 +105,7 @@ __global__ __launch_bounds__(64 * WAVES) void w4_row_kernel(DsqW4Args a, int KS,
                 const int u = u0 + 64 * WAVES * i, k = 128 * first + 8 * u;
                 if (u >= units) break;
                 if (XT != DSQ_T_I8 && k + 8 > a.K) load_frag<XT, false>(f[i], a.x, k, a.K, true);
+                scale_up(f[i]);
                 char *to = lds + 8 * u * L::ES;
                 if constexpr (XT == DSQ_T_F32) {
                     bf16x8 t[3];
@@ -148,6 +149,7 @@ __global__ __launch_bounds__(64 * WAVES) void w4_row_kernel(DsqW4Args a, int KS,
     }
     const int n = 16 * nt + r;
     if (mine >= tiles || n >= a.N || lane >= 16) return;
+    if (XT == DSQ_T_F32) sum *= kDown;
     if constexpr (kSumsOverflow<XT>)
         if (__builtin_expect(overflowed(sum), 0)) sum = product_in_64_bits<XT>(0, n);
     if (XT == DSQ_T_I8) sum *= a.x_scale[0];

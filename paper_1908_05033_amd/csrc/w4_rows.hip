@@ -38,7 +38,9 @@ __device__ __forceinline__ void step(const uint32_t (&w)[NT], const Frag<XT> &x,
     } else if constexpr (XT == DSQ_T_F32) {
         const bf16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
         bf16x8 t[3], c[NT];
-        split3(x.v, t);
+        Frag<XT> up = x;
+        scale_up(up);
+        split3(up.v, t);
 #pragma unroll
         for (int n = 0; n < NT; ++n) c[n] = codes_bf16(w[n]);
 #pragma unroll
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(DsqW4Args a)
             const int64_t m = m0 + 4 * q + c;
             if (m >= a.M) continue;
             if (kSumsOverflow<XT>) again |= overflowed(v[c]) ? 1u << c : 0u;
-            float o = XT == DSQ_T_I8 ? v[c] * a.x_scale[m] : v[c];
+            float o = XT == DSQ_T_I8 ? v[c] * a.x_scale[m] : XT == DSQ_T_F32 ? v[c] * kDown : v[c];
             if (a.bias) o += bias;
             store_out(a.out, m * a.out_stride + n, a.out_type, o);
         }

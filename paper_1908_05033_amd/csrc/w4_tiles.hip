@@ -145,6 +145,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
             } else {
                 Frag<XT> f;
                 __builtin_memcpy(&f, &xr[j], sizeof f);
+                scale_up(f);
                 if constexpr (XT == DSQ_T_F32) {
                     bf16x8 t[3];
                     split3(f.v, t);
@@ -338,7 +339,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void w4_tiles_kernel(DsqW4Args a, 
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    float o = INT ? s[c] * scale[4 * j + c] : s[c];
+                    float o = INT ? s[c] * scale[4 * j + c] : XT == DSQ_T_F32 ? s[c] * kDown : s[c];
                     if (a.bias) o += bias;
                     if (kSumsOverflow<XT>) mark = __builtin_fmaf(s[c], 0.0f, mark);
                     if (8 * WK * j + c < live) out[(8 * WK * j + c) * a.out_stride] = (E)o;

@@ -37,6 +37,30 @@ def test_large_numbers_at_the_end_of_a_row(M, N, K):
         check_some(run_w4(x.to(dt), p, N, K, group), x.to(dt), c, s, z, group)
 
 
+@pytest.mark.parametrize("M,N", SHAPES_F32)
+@pytest.mark.parametrize("K,group", [(300, 64), (1024, 128), (100, 32), (7, 32)])
+def test_binary32_numbers_below_the_parts_that_bfloat16_holds(M, N, K, group):
+    c, s, z = random_w4(M, N, K, group)
+    for up in (1.0, 2.0 ** 60):
+        p = pack(c, s * np.float32(up), z, group)
+        for f in (1e-33, 1e-35, 1e-37, 1e-38, 1e-40, 1e-43, 0.0):
+            x = normal(M, M, K).double().mul(f).float()
+            check_some(run_w4(x, p, N, K, group), x, c, s * np.float32(up), z, group)
+
+
+@pytest.mark.parametrize("M,N", SHAPES_F32)
+def test_small_and_ordinary_binary32_numbers_side_by_side(M, N):
+    """A row of ordinary numbers beside rows of tiny ones, and tiny numbers in ordinary rows."""
+    K, group = 520, 64
+    c, s, z = random_w4(M, N, K, group)
+    p = pack(c, s, z, group)
+    x = normal(1, M, K).double()
+    x[::2] *= 1e-37
+    x[1::2, ::3] *= 1e-39
+    x = x.float()
+    check_some(run_w4(x, p, N, K, group), x, c, s, z, group)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K,group", [(300, 64), (1024, 128), (100, 32), (7, 32)])
 def test_sums_of_codes_past_the_range(dtype, K, group):
