@@ -378,7 +378,8 @@ dsq_status dsq_conv2d_plan(const dsq_conv_desc *d, int chained, float l_a,
  *   row that repeats).  Zero rows are no error: such a call does nothing.
  *   At most 2^21 rows, rows of at most 2^20 elements, 2^24 output channels, 2^36 weights;
  *   DSQ_ERR_UNSUPPORTED beyond, as for an unknown type or group size.
- *   An input that holds an infinity or a NaN makes its own row NaN or infinite and no other.
+ *   An input row that holds an infinity or a NaN spoils its own row of the result, which then
+ *   holds NaN or infinities, and no other (and a weight's gradient, a sum over the rows).
  *
  * Rows of 8-bit codes: int8 [rows][dsq_code_row_bytes(dim)], codes -127..127, the row's
  *   length rounded up to a multiple of 128 with code 0 behind the last; the value a code
@@ -459,11 +460,11 @@ dsq_status dsq_rms_norm_bwd(const void *h, int64_t h_stride, const void *weight,
  * w          device, float32 [N][K]; NULL if codes is given
  * codes      device, uint8 [N][K] (above 15: stored as 15), or NULL
  * scale, zero   device, float32 and uint8 (above 15: 15) [N][ceil(K / group)]; both or, with
- *            w, neither.  A scale is kept to 20 significant bits.
+ *            w, neither.  A scale is kept to 20 significant bits (and to multiples of 2^-145).
  * With w alone each group gets, in binary32, the range from min(w, 0) to max(w, 0):
  *     scale = (max - min) / 15, kept to 20 bits;  zero = rint(-min / scale)
  * and with w in any case  code = clamp(rint(w / scale) + zero, 0, 15); a scale of 0 has
- * code = zero.  Weights and scales are finite numbers.
+ * code = zero.  Weights and scales are finite numbers below 2^126 in size.
  */
 dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
                                const float *scale, const uint8_t *zero, int N, int K,
@@ -477,7 +478,7 @@ dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
  * parts), sums are binary32, and the result is rounded to dtype once.  The zero point's
  * share is formed from the group's sum of x, so sums reach 15 times that of |x|.  A result
  * whose sums pass the range of binary32 on the way is formed again in binary64: rows of
- * finite numbers give what the formula does, some hundred times slower from about 1e34
+ * finite numbers give what the formula does, some hundred times slower from about 1e35
  * (bfloat16) and 1e28 (float32) on.
  * x          device, [M] rows of K elements of dtype
  * bias       device, [N] of dtype, or NULL

@@ -16,7 +16,8 @@ constexpr int RUN = 8;       // blocks of a workgroup
 
 __device__ __forceinline__ float cut_scale(float s)
 {
-    // the low four bits of the word hold the zero point: rounded to nearest, the step is at most 2^-20 of the scale off
+    // the low four bits of the word hold the zero point: rounded to nearest, the step is at most 2^-20 of the scale off.  A lane
+    // reads one word a group for both; what a group of 4-bit codes loses anyway, half a step, is 2^15 times as much.
     return __uint_as_float((__float_as_uint(s) + 8u) & ~15u);
 }
 

@@ -33,7 +33,9 @@ int w4_least_time(int M, int N, const W4Choice (&of)[COUNT])
 }
 
 // A large tile reads least and unpacks a code for most rows, a small one leaves no compute unit idle.  The times of a round are
-// measured at K = 4096 and groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K scales all alike.
+// measured at K = 4096 and groups of 128, in microseconds with bfloat16 rows / 8-bit rows; another K and other groups are taken to scale
+// all alike, which is not measured.  A round is one workgroup a compute unit, though two of the 8-bit 32x64 tile share one (its last
+// lines below take less than rounds times time; larger tiles are ahead there).
 //
 //   rows x N        32x64      64x64      64x128     64x256     128x256
 //   128 x 4096      14 / 9     20 / 12    25 / 17    37 / 26    63 / 40

@@ -10,7 +10,7 @@
 // segment of input channels at a time, shared by the workgroup's waves.  Fifteen of the sixteen rows of a matrix instruction go to
 // waste; it still takes a quarter of the time that its codes take from memory.
 //
-// Measured with bfloat16 rows and groups of 128: 8192 to 32768 channels 28.2 us (5.1 TB/s), 4096 to 4096 4.0 us, a launch and one
+// Measured with bfloat16 rows and groups of 128: 8192 to 32768 channels 28.2 us (5.1 TB/s), 4096 to 4096 4.1 us, a launch and one
 // round of memory latency.
 #include "w4_device.h"
 
