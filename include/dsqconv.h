@@ -464,7 +464,8 @@ dsq_status dsq_rms_norm_bwd(const void *h, int64_t h_stride, const void *weight,
  * With w alone each group gets, in binary32, the range from min(w, 0) to max(w, 0):
  *     scale = (max - min) / 15, kept to 20 bits;  zero = rint(-min / scale)
  * and with w in any case  code = clamp(rint(w / scale) + zero, 0, 15); a scale of 0 has
- * code = zero.  Weights and scales are finite numbers below 2^126 in size.
+ * code = zero.  Weights and scales are finite numbers below 2^96 in size (sums of scaled groups
+ * stay inside binary32).
  */
 dsq_status dsq_pack_weights_w4(const float *w, const uint8_t *codes,
                                const float *scale, const uint8_t *zero, int N, int K,
