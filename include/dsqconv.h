@@ -501,6 +501,169 @@ dsq_status dsq_linear_w4a8(const int8_t *codes, size_t codes_bytes,
                            const void *bias, dsq_dtype dtype, void *out,
                            int64_t out_stride, void *hip_stream);
 
+/* ---- heads ---------------------------------------------------------------------
+ * What lies between the q/k/v product of a block and its output product: norms of the heads
+ * and their rotation by positions, attention over prompts, attention over a paged cache.
+ *
+ *   Heads are [rows][heads][dim] of dtype, the elements of a head side by side, with any
+ *   distance from row to row and from head to head (`_row`, `_head`, in elements, multiples of
+ *   16 bytes, 0 for one that repeats): the parts of one q/k/v tensor are such inputs and such
+ *   outputs.  Heads of an output do not overlap (DSQ_ERR_SHAPE).  q_heads is a multiple of
+ *   kv_heads; query head i uses key head i / (q_heads / kv_heads).  dim is a multiple of 8, at
+ *   most 128 (256 for norm and rotation), and there are at most 1024 heads and 2^16 sequences:
+ *   DSQ_ERR_UNSUPPORTED beyond.
+ *   Packed sequences lie one behind the other: sequence s has the rows starts[s] ..
+ *   starts[s + 1] - 1 (int32 [sequences + 1], not falling); rows of outputs before the first and
+ *   behind the last sequence are left as they were.  Starts outside the rows are taken
+ *   as the nearest end.
+ *   A paged cache is two tensors [pages][kv_heads][page][dim], keys and values; page is a power
+ *   of two up to 2^16.
+ *   Sums, softmax and products are binary32; probabilities (and in the backward pass ds) are rounded
+ *   to dtype where they meet values in the matrix instruction.
+ */
+size_t dsq_qk_norm_rope_bwd_bytes(int rows, int q_heads, int kv_heads, int dim);
+size_t dsq_attention_bwd_bytes(int q_rows, int q_heads);
+size_t dsq_attention_cache_bytes(int sequences, int max_rows, int q_heads, int kv_heads,
+                                 int dim);
+
+/* ---- dsq_qk_norm_rope: norms of the heads, rotation, writing of the cache -------------
+ *     n  = x * weight / sqrt(mean of x^2 + eps)     over a head; n = x with eps = 0
+ *     a' = a cos t - b sin t,  b' = b cos t + a sin t       for each pair j of a head,
+ *                              t = positions[axis of j][row] * frequencies[j]
+ * The first rope_dim elements of a head are rotated (a multiple of 16, 0 for none), the others
+ * pass.  Pair j is the elements j and j + rope_dim / 2, or 2j and 2j + 1 (interleaved != 0).
+ * Angles are formed in binary64, everything else in binary32, rounded to dtype once.
+ *
+ * q, k       device, heads; one may be NULL with 0 heads
+ * v          device, [rows][kv_heads] heads that go to the cache as they are; else unused
+ * q_weight, k_weight   device, [dim] of dtype, or NULL for ones; NULL with eps = 0
+ * eps        finite, >= 0 (DSQ_ERR_RANGE); 0: no norm
+ * positions  device, int32 [axes][rows] (axes 1 .. 16)
+ * pair_axis  device, uint8 [rope_dim / 2]: the axis of each pair (one past the last counts as the
+ *            last), or NULL: axis 0
+ * frequencies   device, float32 [rope_dim / 2]
+ * q_out, k_out  device, out; may be the memory of q and k with the same distances; k_out may
+ *            be NULL if there is a cache
+ * k_cache, v_cache, slots   all or none; slots: device, int64 [rows], page * (page size) + place:
+ *            where a row's keys and values go; rows of a slot outside the cache are not
+ *            written there.  Of two rows with one slot any elements may remain.
+ */
+dsq_status dsq_qk_norm_rope(const void *q, int64_t q_row, int64_t q_head, const void *k,
+                            int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                            int64_t v_head, dsq_dtype dtype, int rows, int q_heads,
+                            int kv_heads, int dim, const void *q_weight,
+                            const void *k_weight, float eps, const int32_t *positions,
+                            int axes, const uint8_t *pair_axis, const float *frequencies,
+                            int rope_dim, int interleaved, void *q_out, int64_t q_out_row,
+                            int64_t q_out_head, void *k_out, int64_t k_out_row,
+                            int64_t k_out_head, void *k_cache, void *v_cache,
+                            int64_t pages, int page, const int64_t *slots,
+                            void *hip_stream);
+
+/* ---- dsq_qk_norm_rope_bwd -------------------------------------------------------
+ * From gradients of q_out and k_out to those of q, k and the weights; q and k are the inputs of
+ * the forward call (unused, but not NULL, with eps = 0).  No atomics: the same result every time.
+ *
+ * grad_q, grad_k   device, out; may be the memory of q, k, grad_q_out or grad_k_out with the same
+ *            distances
+ * grad_q_weight, grad_k_weight   device, out, float32 [dim], or NULL; overwritten (zeros for zero
+ *            rows); NULL with eps = 0
+ * workspace  device, dsq_qk_norm_rope_bwd_bytes(..) bytes, needed for gradients of weights alone;
+ *            of no other call that may run at the same time, captured graphs included
+ */
+dsq_status dsq_qk_norm_rope_bwd(const void *q, int64_t q_row, int64_t q_head,
+                                const void *k, int64_t k_row, int64_t k_head,
+                                dsq_dtype dtype, int rows, int q_heads, int kv_heads,
+                                int dim, const void *q_weight, const void *k_weight,
+                                float eps, const int32_t *positions, int axes,
+                                const uint8_t *pair_axis, const float *frequencies,
+                                int rope_dim, int interleaved, const void *grad_q_out,
+                                int64_t grad_q_out_row, int64_t grad_q_out_head,
+                                const void *grad_k_out, int64_t grad_k_out_row,
+                                int64_t grad_k_out_head, void *grad_q,
+                                int64_t grad_q_row, int64_t grad_q_head, void *grad_k,
+                                int64_t grad_k_row, int64_t grad_k_head,
+                                float *grad_q_weight, float *grad_k_weight,
+                                void *workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
+/* ---- dsq_attention: whole prompts ---------------------------------------------------
+ *     out_i = sum over visible keys j of softmax_j(scale * q_i . k_j) v_j
+ * Row i of a sequence of n rows and m keys sees all m (causal = 0) or those with
+ * j <= i + m - n (causal != 0: its last row sees all).  A row that sees no key is zeros.  What a row
+ * does not see has no part in it, infinities and NaN included.
+ *
+ * q_starts, k_starts   device; k_starts NULL: as q_starts; both NULL: one sequence of all rows
+ *            (sequences = 1)
+ * scale      finite and > 0 (DSQ_ERR_RANGE); scores scale * q . k stay inside binary32
+ * lse        device, out, float32 [q_heads][q_rows]: log of the sum of exp(scale * q . k), -inf for
+ *            a row that sees no key, for the backward pass; or NULL
+ */
+dsq_status dsq_attention(const void *q, int64_t q_row, int64_t q_head, const void *k,
+                         int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                         int64_t v_head, dsq_dtype dtype, int q_rows, int k_rows,
+                         int q_heads, int kv_heads, int dim, const int32_t *q_starts,
+                         const int32_t *k_starts, int sequences, int causal, float scale,
+                         void *out, int64_t out_row, int64_t out_head, float *lse,
+                         void *hip_stream);
+
+/* ---- dsq_attention_bwd --------------------------------------------------------------
+ * From the gradient of out to those of q, k and v, with out and lse as dsq_attention wrote them.
+ * Gradients of a key head are the sums over the query heads that share it.  No atomics: the same
+ * result every time.  An infinity or NaN spoils the gradients of its own sequence and of no other.
+ * In float16 products ds = p * (grad_out . v - out . grad_out) below 2^-14 lose digits and below
+ * 2^-25 vanish: such programs scale their loss.
+ *
+ * grad_q, grad_k, grad_v   device, out; overlap no input
+ * workspace  device, dsq_attention_bwd_bytes(q_rows, q_heads) bytes; of no other call that may
+ *            run at the same time, captured graphs included
+ */
+dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const void *k,
+                             int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                             int64_t v_head, const void *out, int64_t out_row,
+                             int64_t out_head, const float *lse, const void *grad_out,
+                             int64_t grad_out_row, int64_t grad_out_head,
+                             dsq_dtype dtype, int q_rows, int k_rows, int q_heads,
+                             int kv_heads, int dim, const int32_t *q_starts,
+                             const int32_t *k_starts, int sequences, int causal,
+                             float scale, void *grad_q, int64_t grad_q_row,
+                             int64_t grad_q_head, void *grad_k, int64_t grad_k_row,
+                             int64_t grad_k_head, void *grad_v, int64_t grad_v_row,
+                             int64_t grad_v_head, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+
+/* ---- dsq_attention_cache: single tokens and trees of drafted tokens --------------------
+ * The last tokens of each sequence, over all of its keys in the cache, their own included (they
+ * are written there first: dsq_qk_norm_rope).  A sequence of n rows and length m has the keys
+ * 0 .. m - 1; its rows are the tokens m - n .. m - 1, and each sees all keys before m - n and of the
+ * others, drafted key b = 0 .. n - 1, those before it and itself (tree NULL), or those whose bit is
+ * set in its mask (its own bit too, if it sees itself).  A row that sees no key is zeros, and what a
+ * row does not see has no part in it.
+ *
+ * q          device, [rows][q_heads] heads
+ * q_starts   device, or NULL: one row a sequence (rows = sequences)
+ * max_rows   the most rows of a sequence; rows past it in theirs are left as they were
+ * page_table device, int32 [sequences] rows of table_pages pages, table_row apart: key j of a
+ *            sequence is in page page_table[j / page], place j % page.  Keys of a page number
+ *            outside the cache are seen by no row.
+ * lengths    device, int32 [sequences], at most table_pages * page (more counts as that)
+ * tree       device, uint64 [rows][tree_words]: bit b % 64 of word b / 64; keys past the last word are
+ *            not seen; or NULL
+ * workspace  device, dsq_attention_cache_bytes(..) bytes; of no other call that may run at the same
+ *            time, captured graphs included
+ * A sequence has at most 2^30 keys (table_pages * page).
+ */
+dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head,
+                               dsq_dtype dtype, int rows, int q_heads, int kv_heads,
+                               int dim, const int32_t *q_starts, int sequences,
+                               int max_rows, const void *k_cache, const void *v_cache,
+                               int64_t pages, int page, const int32_t *page_table,
+                               int64_t table_row, int table_pages,
+                               const int32_t *lengths, const uint64_t *tree,
+                               int tree_words, float scale, void *out, int64_t out_row,
+                               int64_t out_head, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *dsq_status_string(dsq_status s);
 

@@ -39,6 +39,8 @@ EXPORTS = [
     "dsq_conv2d_plan", "dsq_status_string",
     "dsq_code_row_bytes", "dsq_rms_norm_bwd_bytes", "dsq_w4_packed_bytes", "dsq_w4_scale_bytes",
     "dsq_rms_norm", "dsq_rms_norm_bwd", "dsq_pack_weights_w4", "dsq_linear_w4", "dsq_linear_w4a8",
+    "dsq_qk_norm_rope_bwd_bytes", "dsq_attention_bwd_bytes", "dsq_attention_cache_bytes",
+    "dsq_qk_norm_rope", "dsq_qk_norm_rope_bwd", "dsq_attention", "dsq_attention_bwd", "dsq_attention_cache",
 ]
 
 
@@ -106,6 +108,19 @@ def load_library():
     lib.dsq_rms_norm.argtypes = [vp, i64, vp, i64, vp, i, i, i, f, vp, vp, vp, sz, vp, vp, vp]
     lib.dsq_rms_norm_bwd.restype = i
     lib.dsq_rms_norm_bwd.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, i, i, i, vp, vp, vp, sz, vp]
+    heads = [vp, i64, i64]
+    for name, args in (("dsq_qk_norm_rope_bwd_bytes", [i] * 4), ("dsq_attention_bwd_bytes", [i] * 2), ("dsq_attention_cache_bytes", [i] * 5)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = args
+    rotation = [vp, vp, f, vp, i, vp, vp, i, i]
+    for name, args in (
+            ("dsq_qk_norm_rope", heads * 3 + [i] * 5 + rotation + heads * 2 + [vp, vp, i64, i, vp, vp]),
+            ("dsq_qk_norm_rope_bwd", heads * 2 + [i] * 5 + rotation + heads * 4 + [vp, vp, vp, sz, vp]),
+            ("dsq_attention", heads * 3 + [i] * 6 + [vp, vp, i, i, f] + heads + [vp, vp]),
+            ("dsq_attention_bwd", heads * 4 + [vp] + heads + [i] * 6 + [vp, vp, i, i, f] + heads * 3 + [vp, sz, vp]),
+            ("dsq_attention_cache", heads + [i] * 5 + [vp, i, i, vp, vp, i64, i, vp, i64, i, vp, vp, i, f] + heads + [vp, sz, vp])):
+        getattr(lib, name).restype = i
+        getattr(lib, name).argtypes = args
     lib.dsq_pack_weights_w4.restype = i
     lib.dsq_pack_weights_w4.argtypes = [vp, vp, vp, vp, i, i, i, vp, sz, vp, sz, vp]
     lib.dsq_linear_w4.restype = i
@@ -130,6 +145,7 @@ class _NoMarshal:
 
     conv2d = conv2d_requant = conv2d_wq = soft_quantize_fwd = soft_quantize_bwd = quantize_act
     rms_norm = rms_norm_bwd = linear_w4 = linear_w4a8 = quantize_act
+    qk_norm_rope = qk_norm_rope_bwd = attention = attention_bwd = attention_cache = quantize_act
 
 
 def load_marshal():
@@ -152,6 +168,8 @@ def load_marshal():
         module.init_lm(*(C.cast(getattr(lib, name), C.c_void_p).value for name in
                          ("dsq_rms_norm", "dsq_rms_norm_bwd", "dsq_linear_w4", "dsq_linear_w4a8", "dsq_code_row_bytes",
                           "dsq_w4_packed_bytes", "dsq_w4_scale_bytes")))
+        module.init_heads(*(C.cast(getattr(lib, name), C.c_void_p).value for name in
+                            ("dsq_qk_norm_rope", "dsq_qk_norm_rope_bwd", "dsq_attention", "dsq_attention_bwd", "dsq_attention_cache")))
         _marshal = module
     return _marshal
 
@@ -473,6 +491,191 @@ def dsq_linear_w4a8(codes, scales, w_packed, w_scales, N, K, group, bias, out, s
     wp, sp = _packed(w_packed, w_scales, N, K, group)
     _check(load_library().dsq_linear_w4a8(cp, codes.numel(), _vector(scales, "scales", M, torch.float32), M, N, K, group, wp, sp,
                                           _vector(bias, "bias", N, out.dtype, True), _DTYPES[out.dtype], op, os_, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Heads of a block: tensors [rows, heads, dim] whose rows and heads may lie apart (stride(2) is 1).
+# ---------------------------------------------------------------------------
+
+def dsq_qk_norm_rope_bwd_bytes(rows, q_heads, kv_heads, dim):
+    return int(load_library().dsq_qk_norm_rope_bwd_bytes(rows, q_heads, kv_heads, dim))
+
+
+def dsq_attention_bwd_bytes(q_rows, q_heads):
+    return int(load_library().dsq_attention_bwd_bytes(q_rows, q_heads))
+
+
+def dsq_attention_cache_bytes(sequences, max_rows, q_heads, kv_heads, dim):
+    return int(load_library().dsq_attention_cache_bytes(sequences, max_rows, q_heads, kv_heads, dim))
+
+
+def _heads(t, name, shape=None, dtype=None, allow_none=False):
+    """(address, distance of rows, distance of heads) of a tensor [rows, heads, dim]; zeros where it may be None.
+    Entries of the shape that are None are not compared."""
+    if t is None and allow_none:
+        return None, 0, 0
+    _here(t, name)
+    if t.dim() != 3 or (shape is not None and any(n is not None and n != m for n, m in zip(shape, t.shape))):
+        raise DsqError(4, "%s has the shape %s%s" % (name, list(t.shape), "" if shape is None else ", expected %s" % list(shape)))
+    if t.dtype not in _DTYPES if dtype is None else t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, "float32, float16 or bfloat16" if dtype is None else dtype, t.dtype))
+    rows, heads, dim = t.shape
+    if t.numel() and dim > 1 and t.stride(2) != 1:
+        raise TypeError("%s: the elements of a head must lie side by side" % name)
+    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dim, t.stride(1) if heads > 1 else dim
+
+
+def _rotation(positions, rows, pair_axis, frequencies):
+    """positions, axes, pair_axis, frequencies, rope_dim as the library takes them."""
+    pairs = frequencies.numel() if isinstance(frequencies, torch.Tensor) else 0
+    axes = positions.shape[0] if isinstance(positions, torch.Tensor) and positions.dim() == 2 else 1
+    return (_vector(positions, "positions", axes * rows, torch.int32, True), axes, _vector(pair_axis, "pair_axis", pairs, torch.uint8, True),
+            _vector(frequencies, "frequencies", pairs, torch.float32, True), 2 * pairs)
+
+
+def _both(q, k):
+    """rows, query heads, key heads, dim and type of q and k, one of which may be None."""
+    one = q if q is not None else k
+    _heads(one, "q")
+    rows, heads, dim = one.shape
+    if q is not None and k is not None:
+        _heads(k, "k", (rows, None, dim), q.dtype)
+    return rows, 0 if q is None else heads, 0 if k is None else k.shape[1], dim, one.dtype
+
+
+def dsq_qk_norm_rope(q, k, v, q_weight, k_weight, eps, positions, pair_axis, frequencies, interleaved, q_out, k_out, k_cache, v_cache,
+                     slots, stream=None):
+    """q [rows, q_heads, dim], k and v [rows, kv_heads, dim]; weights [dim]; positions int32 [rows] or [axes, rows]; frequencies
+    float32 and pair_axis uint8 [rope_dim / 2]; caches [pages, kv_heads, page, dim]; slots int64 [rows].  What is not wanted is None."""
+    status = (_marshal or load_marshal()).qk_norm_rope(q, k, v, q_weight, k_weight, eps, positions, pair_axis, frequencies, interleaved, q_out,
+                                                       k_out, k_cache, v_cache, slots, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
+    rows, hq, hk, dim, dt = _both(q, k)
+    pages, page = 0, 0
+    if k_cache is not None:
+        pages, page = _cache(k_cache, "k_cache", hk, dim, dt)
+        if v_cache is not None and _cache(v_cache, "v_cache", hk, dim, dt) != (pages, page):
+            raise DsqError(4, "k_cache and v_cache have different shapes")
+    elif v_cache is not None or slots is not None:
+        raise DsqError(1, "k_cache is a required tensor where v_cache or slots is given")
+    _check(load_library().dsq_qk_norm_rope(
+        *_heads(q, "q", allow_none=True), *_heads(k, "k", allow_none=True), *_heads(v, "v", (rows, hk, dim), dt, True), _DTYPES[dt], rows, hq, hk, dim,
+        _vector(q_weight, "q_weight", dim, dt, True), _vector(k_weight, "k_weight", dim, dt, True), eps,
+        *_rotation(positions, rows, pair_axis, frequencies), int(bool(interleaved)), *_heads(q_out, "q_out", (rows, hq, dim), dt, True),
+        *_heads(k_out, "k_out", (rows, hk, dim), dt, True), None if k_cache is None else k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), pages, page, _vector(slots, "slots", rows, torch.int64, True), _stream(stream)))
+
+
+def dsq_qk_norm_rope_bwd(q, k, q_weight, k_weight, eps, positions, pair_axis, frequencies, interleaved, grad_q_out, grad_k_out, grad_q, grad_k,
+                         grad_q_weight, grad_k_weight, workspace, stream=None):
+    """As dsq_qk_norm_rope; gradients in the shapes of q and k; of the weights float32 [dim] or None; workspace uint8 of
+    dsq_qk_norm_rope_bwd_bytes(..)."""
+    status = (_marshal or load_marshal()).qk_norm_rope_bwd(q, k, q_weight, k_weight, eps, positions, pair_axis, frequencies, interleaved, grad_q_out, grad_k_out,
+                                                           grad_q, grad_k, grad_q_weight, grad_k_weight, workspace, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
+    rows, hq, hk, dim, dt = _both(q, k)
+    like = lambda t, name, heads: _heads(t, name, (rows, heads, dim), dt, heads == 0)
+    ws, nbytes = _bytes(workspace, "workspace", True)
+    _check(load_library().dsq_qk_norm_rope_bwd(
+        *_heads(q, "q", allow_none=True), *_heads(k, "k", allow_none=True), _DTYPES[dt], rows, hq, hk, dim,
+        _vector(q_weight, "q_weight", dim, dt, True), _vector(k_weight, "k_weight", dim, dt, True), eps,
+        *_rotation(positions, rows, pair_axis, frequencies), int(bool(interleaved)), *like(grad_q_out, "grad_q_out", hq),
+        *like(grad_k_out, "grad_k_out", hk), *like(grad_q, "grad_q", hq), *like(grad_k, "grad_k", hk),
+        _vector(grad_q_weight, "grad_q_weight", dim, torch.float32, True), _vector(grad_k_weight, "grad_k_weight", dim, torch.float32, True),
+        ws, nbytes, _stream(stream)))
+
+
+def _prompts(q, k, v, q_starts, k_starts):
+    """Rows, keys, heads, dim, type, addresses of the starts and the number of sequences."""
+    _heads(q, "q")
+    (rows, hq, dim), dt = q.shape, q.dtype
+    _heads(k, "k", (None, None, dim), dt)
+    _heads(v, "v", k.shape, dt)
+    sequences = 1
+    if q_starts is not None:
+        sequences = max(0, _here(q_starts, "q_starts").numel() - 1)
+    starts = [_vector(t, name, sequences + 1, torch.int32, True) for t, name in ((q_starts, "q_starts"), (k_starts, "k_starts"))]
+    return rows, k.shape[0], hq, k.shape[1], dim, dt, starts, sequences
+
+
+def dsq_attention(q, k, v, q_starts, k_starts, causal, scale, out, lse, stream=None):
+    """q, out [rows, q_heads, dim]; k, v [keys, kv_heads, dim]; starts int32 [sequences + 1] or None; lse float32 [q_heads, rows] or None."""
+    status = (_marshal or load_marshal()).attention(q, k, v, q_starts, k_starts, causal, scale, out, lse, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
+    rows, keys, hq, hk, dim, dt, starts, sequences = _prompts(q, k, v, q_starts, k_starts)
+    _check(load_library().dsq_attention(
+        *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), _DTYPES[dt], rows, keys, hq, hk, dim, *starts, sequences, int(bool(causal)), scale,
+        *_heads(out, "out", q.shape, dt), _vector(lse, "lse", hq * rows, torch.float32, True), _stream(stream)))
+
+
+def dsq_attention_bwd(q, k, v, out, lse, grad_out, q_starts, k_starts, causal, scale, grad_q, grad_k, grad_v, workspace, stream=None):
+    """As dsq_attention, with its out and lse; gradients in the shapes of what they belong to; workspace uint8 of
+    dsq_attention_bwd_bytes(rows, q_heads)."""
+    status = (_marshal or load_marshal()).attention_bwd(q, k, v, out, lse, grad_out, q_starts, k_starts, causal, scale, grad_q, grad_k,
+                                                        grad_v, workspace, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
+    rows, keys, hq, hk, dim, dt, starts, sequences = _prompts(q, k, v, q_starts, k_starts)
+    ws, nbytes = _bytes(workspace, "workspace", True)
+    _check(load_library().dsq_attention_bwd(
+        *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(out, "out", q.shape, dt), _vector(lse, "lse", hq * rows, torch.float32),
+        *_heads(grad_out, "grad_out", q.shape, dt), _DTYPES[dt], rows, keys, hq, hk, dim, *starts, sequences, int(bool(causal)), scale,
+        *_heads(grad_q, "grad_q", q.shape, dt), *_heads(grad_k, "grad_k", k.shape, dt), *_heads(grad_v, "grad_v", k.shape, dt),
+        ws, nbytes, _stream(stream)))
+
+
+def _cache(t, name, heads, dim, dtype):
+    """Pages and page size of a cache [pages, heads, page, dim]."""
+    if _here(t, name).dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 4 or t.shape[1] != heads or t.shape[3] != dim:
+        raise DsqError(4, "%s has the shape %s, expected [pages, %d, page, %d]" % (name, list(t.shape), heads, dim))
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    return t.shape[0], t.shape[2]
+
+
+def dsq_attention_cache(q, q_starts, max_rows, k_cache, v_cache, page_table, lengths, tree, scale, out, workspace, stream=None):
+    """q, out [rows, q_heads, dim]; q_starts int32 [sequences + 1] or None; caches [pages, kv_heads, page, dim]; page_table int32
+    [sequences, pages of each] whose rows may lie apart; lengths int32 [sequences]; tree int64 [rows, words] or None; workspace uint8 of
+    dsq_attention_cache_bytes(sequences, max_rows, q_heads, kv_heads, dim)."""
+    status = (_marshal or load_marshal()).attention_cache(q, q_starts, max_rows, k_cache, v_cache, page_table, lengths, tree, scale, out, workspace, stream)
+    if status is not None:
+        if status != DSQ_OK:
+            _check(status)
+        return
+    qp = _heads(q, "q")
+    (rows, hq, dim), dt = q.shape, q.dtype
+    if _here(k_cache, "k_cache").dim() != 4:
+        raise DsqError(4, "k_cache has the shape %s, expected [pages, kv_heads, page, dim]" % list(k_cache.shape))
+    hk = k_cache.shape[1]
+    pages, page = _cache(k_cache, "k_cache", hk, dim, dt)
+    if _cache(v_cache, "v_cache", hk, dim, dt) != (pages, page):
+        raise DsqError(4, "k_cache and v_cache have different shapes")
+    sequences = _here(lengths, "lengths").numel()
+    tp, tr = _rows(page_table, "page_table", (sequences, page_table.shape[-1]) if isinstance(page_table, torch.Tensor) and page_table.dim() else None,
+                   torch.int32)
+    words = 0
+    if tree is not None:
+        if _here(tree, "tree").dim() != 2 or not tree.shape[1]:
+            raise DsqError(4, "tree has the shape %s, expected [%d, words]" % (list(tree.shape), rows))
+        words = tree.shape[1]
+    ws, nbytes = _bytes(workspace, "workspace")
+    _check(load_library().dsq_attention_cache(
+        *qp, _DTYPES[dt], rows, hq, hk, dim, _vector(q_starts, "q_starts", sequences + 1, torch.int32, True), sequences, max_rows,
+        k_cache.data_ptr(), v_cache.data_ptr(), pages, page, tp, tr, page_table.shape[1], _vector(lengths, "lengths", sequences, torch.int32),
+        _vector(tree, "tree", rows * words, torch.int64, True), words, scale, *_heads(out, "out", q.shape, dt), ws, nbytes, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,232 @@
+// Device-side helpers of the attention kernels (gfx950 only): operands of the 32x32 matrix instructions, tiles in LDS, packed sequences.
+//
+// All products are formed as 32 x 32 tiles.  Lane l of a wave, r = l % 32 and h = l / 32, holds of an operand the eight numbers
+// (r, k = 8h .. 8h + 7) of a step of 16, and of a result the column r and the rows 8 (i / 4) + 4 h + i % 4, i = 0 .. 15.  The numbers
+// i = 8s .. 8s + 7 of a result are therefore an operand of step s of the next product without any exchange between lanes, whose
+// other operand takes its k in the same order: rows 16 s + 4 h + 0 .. 3 and 16 s + 8 + 4 h + 0 .. 3 of a tile ("columns" below).
+#pragma once
+#include "attn_kernels.h"
+#include "lm_device.h"
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v8f __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+template <class E>
+struct Operand {
+    typedef E type __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ v16f multiply(Operand<__bf16>::type a, Operand<__bf16>::type b, v16f c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ v16f multiply(Operand<_Float16>::type a, Operand<_Float16>::type b, v16f c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// binary32: eight products of two steps each, which take k = i of both halves in step i.
+__device__ __forceinline__ v16f multiply(v8f a, v8f b, v16f c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// Numbers 8s .. 8s + 7 of a result as an operand, rounded to the type: a product's operands have its inputs' type.
+template <class E>
+__device__ __forceinline__ typename Operand<E>::type operand_of(const v16f &c, int s)
+{
+    v8f part;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[i] = c[8 * s + i];
+    return __builtin_convertvector(part, typename Operand<E>::type);
+}
+
+// ---- tiles in LDS: rows of HD elements, their 16-byte units exchanged within a row by a function of the row's number, so that
+// neither 16 lanes that read the same unit of 16 rows nor four rows of 64 bytes that are read as columns meet in a bank.
+template <class E, int HD>
+struct Tile {
+    static constexpr int PER = 16 / (int)sizeof(E);          // elements of a unit
+    static constexpr int UNITS = HD / PER;
+    static __device__ __forceinline__ int place(int row, int unit)
+    {
+        const int f = UNITS >= 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        return row * HD + (unit ^ f) * PER;
+    }
+    // (row r, k = 16 s + 8 h .. + 7)
+    static __device__ __forceinline__ typename Operand<E>::type row_operand(const E *t, int row, int s, int h)
+    {
+        typename Operand<E>::type v;
+        if constexpr (sizeof(E) == 2) {
+            v = *reinterpret_cast<const typename Operand<E>::type *>(t + place(row, 2 * s + h));
+        } else {
+            const v4f lo = *reinterpret_cast<const v4f *>(t + place(row, 4 * s + 2 * h));
+            const v4f hi = *reinterpret_cast<const v4f *>(t + place(row, 4 * s + 2 * h + 1));
+            v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return v;
+    }
+    // (column d0 + r, rows k0 + 4 h + 0 .. 3 and k0 + 8 + 4 h + 0 .. 3): 16 lanes read four rows of 16 elements and exchange them
+    static __device__ __forceinline__ typename Operand<E>::type column_operand(const E *t, int k0, int d0, int lane)
+    {
+        typename Operand<E>::type v;
+        if constexpr (sizeof(E) == 2) {
+            const int row = k0 + (lane >> 5) * 4 + (lane >> 2 & 3);
+            const int unit = d0 / 8 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1), in = (lane & 1) * 4;
+            typedef __attribute__((address_space(3))) v4s *lds;
+            union {
+                v4s half[2];
+                typename Operand<E>::type all;
+            } u;
+            u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(t + place(row, unit) + in));
+            u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(t + place(row + 8, unit) + in));
+            v = u.all;
+        } else {
+            const int d = d0 + (lane & 31), row = k0 + (lane >> 5) * 4;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = t[place(row + i % 4 + i / 4 * 8, d / 4) + d % 4];
+        }
+        return v;
+    }
+};
+
+// Lanes of one wave read what others of it wrote to LDS: they do so in order, and the compiler is not to change it.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// One number for both lanes of a column.
+__device__ __forceinline__ float both_max(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_elementwise_maximum(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float both_sum(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+__device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
+// The eight elements from element 8u of a head (zeros past its last and where there is no row), in the order of memory.
+template <class E>
+__device__ __forceinline__ typename Operand<E>::type load_unit8(const E *row, int u, int dim, bool there)
+{
+    typename Operand<E>::type v = {};
+    if (there && u * 8 < dim) {
+        if constexpr (sizeof(E) == 2) {
+            v = *reinterpret_cast<const typename Operand<E>::type *>(row + u * 8);
+        } else {
+            const v4f lo = *reinterpret_cast<const v4f *>(row + u * 8), hi = *reinterpret_cast<const v4f *>(row + u * 8 + 4);
+            v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    return v;
+}
+
+// ---- packed sequences ---------------------------------------------------------------------------
+//
+// Tiles of `tile` rows: sequence s has its own from number starts[s] / tile + s on, which leaves room for as many as it
+// needs without a sum over the sequences before it; tiles past its end have nothing to do.
+struct Sequence {
+    int at, q0, q_len, k0, k_len;            // at: the tile's first row within the sequence; negative: no tile
+};
+
+__device__ __forceinline__ int clamped(int v, int most) { return v < 0 ? 0 : v > most ? most : v; }
+
+// All 64 lanes take part, with the same arguments: the last sequence whose first tile (or, with tile 0, first row) is not behind `number`;
+// negative if there is none.
+__device__ __forceinline__ int find_sequence(const int32_t *starts, int rows, int sequences, int tile, int number)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = sequences;
+    while (true) {
+        const int step = (n + 63) / 64, s = lane * step < n ? lo + lane * step : lo, start = clamped(starts[s], rows);
+        const int count = __popcll(__ballot(lane * step < n && (tile ? start / tile + s : start) <= number));
+        if (count == 0) return -1;
+        lo += (count - 1) * step;
+        n = n - (count - 1) * step < step ? n - (count - 1) * step : step;
+        if (n <= 1) return __builtin_amdgcn_readfirstlane(lo);
+    }
+}
+
+// by_keys: the tiles are of keys.
+__device__ __forceinline__ Sequence tile_of(const int32_t *q_starts, const int32_t *k_starts, int q_rows, int k_rows, int sequences,
+                                            bool by_keys, int tile, int number)
+{
+    Sequence s = {-1, 0, q_rows, 0, k_rows};
+    if (!q_starts) {
+        s.at = number * tile;
+    } else {
+        const int rows = by_keys ? k_rows : q_rows;
+        const int32_t *starts = by_keys ? k_starts : q_starts;
+        const int i = find_sequence(starts, rows, sequences, tile, number);
+        if (i < 0) return s;
+        s.q0 = clamped(q_starts[i], q_rows);
+        s.q_len = clamped(q_starts[i + 1], q_rows) - s.q0;
+        s.k0 = clamped(k_starts[i], k_rows);
+        s.k_len = clamped(k_starts[i + 1], k_rows) - s.k0;
+        if (s.q_len < 0) s.q_len = 0;
+        if (s.k_len < 0) s.k_len = 0;
+        s.at = (number - (by_keys ? s.k0 : s.q0) / tile - i) * tile;
+    }
+    if (s.at >= (by_keys ? s.k_len : s.q_len)) s.at = -1;
+    return s;
+}
+
+// Number of keys that row i of a sequence sees.
+__device__ __forceinline__ int visible(const Sequence &s, int causal, int i)
+{
+    const int n = causal ? i + s.k_len - s.q_len + 1 : s.k_len;
+    return n < 0 ? 0 : n > s.k_len ? s.k_len : n;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// A softmax's reference before its first key: below every score, and finite, so that differences with it are numbers.
+constexpr float kNoKey = -3.0e38f;
+
+// ---- a row formed again ---------------------------------------------------------------------------
+//
+// A masked key counts for nothing, but in a product of whole tiles its zero meets its value, and zero times an infinity or
+// NaN is NaN.  Rows whose result is not finite are therefore formed again from their visible keys alone, by one wave each.
+// Keys: `int count()`, `bool seen(j)`, `const E *key(j)`, `const E *value(j)` for keys that are seen.
+// Leaves the normed row in o (elements lane, lane + 64 of it) and returns the logarithm to base 2 of its sum.
+template <class E, class Keys>
+__device__ __forceinline__ float row_again(const E *q, int dim, float c, const Keys &keys, float o[2])
+{
+    const int lane = threadIdx.x & 63, count = keys.count();
+    auto score = [&](int j) {
+        const E *k = keys.key(j);
+        float s = 0.0f;
+        for (int d = 0; d < dim; ++d) s = __builtin_fmaf((float)q[d], (float)k[d], s);
+        return s * c;
+    };
+    float m = kNoKey;
+    for (int j = lane; j < count; j += 64)
+        if (keys.seen(j)) m = __builtin_elementwise_maximum(m, score(j));
+    for (int off = 32; off > 0; off >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, off));
+    float l = 0.0f;
+    for (int j = lane; j < count; j += 64)
+        if (keys.seen(j)) l += __builtin_amdgcn_exp2f(score(j) - m);
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+    o[0] = o[1] = 0.0f;
+    for (int j0 = 0; j0 < count; j0 += 64) {
+        const int mine = j0 + lane;
+        const bool seen = mine < count && keys.seen(mine);
+        const float p = seen ? __builtin_amdgcn_exp2f(score(mine) - m) / l : 0.0f;
+        uint64_t left = __ballot(seen);
+        while (left) {
+            const int i = __ffsll((unsigned long long)left) - 1;
+            left &= left - 1;
+            const float pi = __shfl(p, i);
+            const E *v = keys.value(j0 + i);
+            if (lane < dim) o[0] = __builtin_fmaf(pi, (float)v[lane], o[0]);
+            if (lane + 64 < dim) o[1] = __builtin_fmaf(pi, (float)v[lane + 64], o[1]);
+        }
+    }
+    return m + __builtin_amdgcn_logf(l);
+}

@@ -18,6 +18,8 @@
 #include <limits.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "../../include/dsqconv.h"
 
 namespace {
@@ -35,6 +37,11 @@ decltype(&dsq_linear_w4a8) f_linear_w4a8;
 decltype(&dsq_code_row_bytes) f_code_row_bytes;
 decltype(&dsq_w4_packed_bytes) f_w4_packed_bytes;
 decltype(&dsq_w4_scale_bytes) f_w4_scale_bytes;
+decltype(&dsq_qk_norm_rope) f_qk_norm_rope;
+decltype(&dsq_qk_norm_rope_bwd) f_qk_norm_rope_bwd;
+decltype(&dsq_attention) f_attention;
+decltype(&dsq_attention_bwd) f_attention_bwd;
+decltype(&dsq_attention_cache) f_attention_cache;
 PyTypeObject *desc_type;
 
 // Reads arguments one after the other; `plain` turns false at the first that is not.
@@ -127,6 +134,48 @@ struct Args {
         if (!t) return nullptr;
         if (t->scalar_type() != type || !t->is_contiguous() || (n >= 0 && t->numel() != n)) { plain = false; return nullptr; }
         return t->data_ptr();
+    }
+    struct Heads {
+        void *p = nullptr;
+        int64_t rows = 0, heads = 0, dim = 0, row = 0, head = 0;
+        at::ScalarType type = at::kFloat;
+        bool none = false;
+    };
+    // [rows, heads, dim] with the elements of a head side by side; `like`: of its shape and type.
+    Heads heads(const Heads *like, bool may_be_none = false)
+    {
+        Heads r;
+        const at::Tensor *t = here(may_be_none);
+        r.none = !t;
+        if (!t) return r;
+        if (t->dim() != 3 || t->size(0) > INT_MAX || t->size(1) > INT_MAX || t->size(2) > INT_MAX) { plain = false; return r; }
+        r.rows = t->size(0); r.heads = t->size(1); r.dim = t->size(2); r.type = t->scalar_type();
+        r.row = r.rows > 1 ? t->stride(0) : r.heads * r.dim;
+        r.head = r.heads > 1 ? t->stride(1) : r.dim;
+        if ((like ? r.rows != like->rows || r.heads != like->heads || r.dim != like->dim || r.type != like->type : dtype(r.type) < 0) ||
+            (t->numel() && r.dim > 1 && t->stride(2) != 1))
+            plain = false;
+        else r.p = t->data_ptr();
+        return r;
+    }
+    struct Cache {
+        void *p = nullptr;
+        int64_t pages = 0, heads = 0, page = 0;
+    };
+    // A cache [pages, heads, page, dim] for heads like `like`.
+    Cache cache(const Heads &like, bool may_be_none = false)
+    {
+        Cache c;
+        const at::Tensor *t = here(may_be_none);
+        if (!t) return c;
+        if (t->dim() != 4 || t->size(3) != like.dim || t->scalar_type() != like.type || !t->is_contiguous() || t->size(2) > INT_MAX ||
+            t->size(1) > INT_MAX) {
+            plain = false;
+            return c;
+        }
+        c.pages = t->size(0); c.heads = t->size(1); c.page = t->size(2);
+        c.p = t->data_ptr();
+        return c;
     }
     void *bytes(size_t &n, bool may_be_none = false)
     {
@@ -396,6 +445,202 @@ PyObject *linear_w4a8(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// positions [rows] or [axes, rows], pair_axis, frequencies, interleaved
+struct Rotation {
+    const int32_t *positions;
+    const uint8_t *pair_axis;
+    const float *frequencies;
+    int axes = 1, rope_dim = 0, interleaved;
+    Rotation(Args &a, int64_t rows)
+    {
+        PyObject *o = a.at[0], *f = a.at[2];
+        const auto tensor = [](PyObject *x) { return THPVariable_CheckTypeExact(Py_TYPE(x)) && THPVariable_Unpack(x).defined(); };
+        if (tensor(o) && THPVariable_Unpack(o).dim() == 2) axes = (int)std::min<int64_t>(THPVariable_Unpack(o).size(0), INT_MAX);
+        int64_t pairs = 0;
+        if (tensor(f)) pairs = THPVariable_Unpack(f).numel();
+        if (pairs > INT_MAX / 2) a.plain = false;
+        positions = (const int32_t *)a.vector(axes * rows, at::kInt, true);
+        pair_axis = (const uint8_t *)a.vector(pairs, at::kByte, true);
+        frequencies = (const float *)a.vector(pairs, at::kFloat, true);
+        rope_dim = (int)(2 * pairs);
+        interleaved = a.truth();
+    }
+};
+
+PyObject *qk_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Args a(args, n, 16);
+        if (!a.plain || !f_qk_norm_rope) Py_RETURN_NONE;
+        const Args::Heads q = a.heads(nullptr), k = a.heads(nullptr), v = a.heads(&k, true);
+        const void *qw = a.vector(q.dim, q.type, true), *kw = a.vector(q.dim, q.type, true);
+        const float eps = a.real();
+        const Rotation r(a, q.rows);
+        const Args::Heads qo = a.heads(&q), ko = a.heads(&k, true);
+        const Args::Cache kc = a.cache(k, true), vc = a.cache(k, true);
+        const int64_t *slots = (const int64_t *)a.vector(q.rows, at::kLong, true);
+        void *stream = a.stream();
+        if (k.rows != q.rows || k.dim != q.dim || k.type != q.type || kc.pages != vc.pages || kc.page != vc.page ||
+            ((kc.p || vc.p) && (kc.heads != k.heads || vc.heads != k.heads)) || ((vc.p || slots) && !kc.p))
+            a.plain = false;
+        return call(a, [=] {
+            return f_qk_norm_rope(q.p, q.row, q.head, k.p, k.row, k.head, v.p, v.row, v.head, (dsq_dtype)Args::dtype(q.type), (int)q.rows,
+                                  (int)q.heads, (int)k.heads, (int)q.dim, qw, kw, eps, r.positions, r.axes, r.pair_axis, r.frequencies,
+                                  r.rope_dim, r.interleaved, qo.p, qo.row, qo.head, ko.p, ko.row, ko.head, kc.p, vc.p, kc.pages,
+                                  (int)kc.page, slots, stream);
+        });
+    });
+}
+
+PyObject *qk_norm_rope_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Args a(args, n, 17);
+        if (!a.plain || !f_qk_norm_rope_bwd) Py_RETURN_NONE;
+        const Args::Heads q = a.heads(nullptr), k = a.heads(nullptr);
+        const void *qw = a.vector(q.dim, q.type, true), *kw = a.vector(q.dim, q.type, true);
+        const float eps = a.real();
+        const Rotation r(a, q.rows);
+        const Args::Heads gqo = a.heads(&q), gko = a.heads(&k), gq = a.heads(&q), gk = a.heads(&k);
+        float *gqw = (float *)a.vector(q.dim, at::kFloat, true), *gkw = (float *)a.vector(q.dim, at::kFloat, true);
+        size_t size;
+        void *ws = a.bytes(size, true), *stream = a.stream();
+        if (k.rows != q.rows || k.dim != q.dim || k.type != q.type) a.plain = false;
+        return call(a, [=] {
+            return f_qk_norm_rope_bwd(q.p, q.row, q.head, k.p, k.row, k.head, (dsq_dtype)Args::dtype(q.type), (int)q.rows, (int)q.heads,
+                                      (int)k.heads, (int)q.dim, qw, kw, eps, r.positions, r.axes, r.pair_axis, r.frequencies, r.rope_dim,
+                                      r.interleaved, gqo.p, gqo.row, gqo.head, gko.p, gko.row, gko.head, gq.p, gq.row, gq.head, gk.p, gk.row,
+                                      gk.head, gqw, gkw, ws, size, stream);
+        });
+    });
+}
+
+// q_starts and k_starts, either of which may be None.
+struct Starts {
+    const int32_t *q, *k;
+    int64_t sequences = 1;
+    explicit Starts(Args &a)
+    {
+        PyObject *o = a.at[0];
+        if (a.plain && o != Py_None && THPVariable_CheckTypeExact(Py_TYPE(o)) && THPVariable_Unpack(o).defined())
+            sequences = THPVariable_Unpack(o).numel() - 1;
+        if (sequences < 0 || sequences > INT_MAX) a.plain = false;
+        q = (const int32_t *)a.vector(sequences + 1, at::kInt, true);
+        k = (const int32_t *)a.vector(sequences + 1, at::kInt, true);
+    }
+};
+
+PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Args a(args, n, 10);
+        if (!a.plain || !f_attention) Py_RETURN_NONE;
+        const Args::Heads q = a.heads(nullptr), k = a.heads(nullptr), v = a.heads(&k);
+        const Starts s(a);
+        const int causal = a.truth();
+        const float scale = a.real();
+        const Args::Heads out = a.heads(&q);
+        float *lse = (float *)a.vector(q.heads * q.rows, at::kFloat, true);
+        void *stream = a.stream();
+        if (k.dim != q.dim || k.type != q.type) a.plain = false;
+        return call(a, [=] {
+            return f_attention(q.p, q.row, q.head, k.p, k.row, k.head, v.p, v.row, v.head, (dsq_dtype)Args::dtype(q.type), (int)q.rows,
+                               (int)k.rows, (int)q.heads, (int)k.heads, (int)q.dim, s.q, s.k, (int)s.sequences, causal, scale, out.p, out.row,
+                               out.head, lse, stream);
+        });
+    });
+}
+
+PyObject *attention_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Args a(args, n, 15);
+        if (!a.plain || !f_attention_bwd) Py_RETURN_NONE;
+        const Args::Heads q = a.heads(nullptr), k = a.heads(nullptr), v = a.heads(&k), out = a.heads(&q);
+        const float *lse = (const float *)a.vector(q.heads * q.rows, at::kFloat);
+        const Args::Heads go = a.heads(&q);
+        const Starts s(a);
+        const int causal = a.truth();
+        const float scale = a.real();
+        const Args::Heads gq = a.heads(&q), gk = a.heads(&k), gv = a.heads(&k);
+        size_t size;
+        void *ws = a.bytes(size, true), *stream = a.stream();
+        if (k.dim != q.dim || k.type != q.type) a.plain = false;
+        return call(a, [=] {
+            return f_attention_bwd(q.p, q.row, q.head, k.p, k.row, k.head, v.p, v.row, v.head, out.p, out.row, out.head, lse, go.p, go.row,
+                                   go.head, (dsq_dtype)Args::dtype(q.type), (int)q.rows, (int)k.rows, (int)q.heads, (int)k.heads, (int)q.dim,
+                                   s.q, s.k, (int)s.sequences, causal, scale, gq.p, gq.row, gq.head, gk.p, gk.row, gk.head, gv.p, gv.row,
+                                   gv.head, ws, size, stream);
+        });
+    });
+}
+
+PyObject *attention_cache(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&] {
+        Args a(args, n, 12);
+        if (!a.plain || !f_attention_cache) Py_RETURN_NONE;
+        const Args::Heads q = a.heads(nullptr);
+        PyObject *o = args[6];                                               // lengths
+        if (!THPVariable_CheckTypeExact(Py_TYPE(o)) || !THPVariable_Unpack(o).defined()) Py_RETURN_NONE;
+        const int64_t sequences = THPVariable_Unpack(o).numel();
+        if (sequences > INT_MAX) Py_RETURN_NONE;
+        const int32_t *starts = (const int32_t *)a.vector(sequences + 1, at::kInt, true);
+        const int max_rows = a.integer();
+        const Args::Cache kc = a.cache(q), vc = a.cache(q);
+        Args::Rows table;
+        if (const at::Tensor *t = a.here(false)) {
+            if (t->dim() != 2 || t->size(0) != sequences || t->size(1) > INT_MAX || t->scalar_type() != at::kInt ||
+                (t->numel() && t->size(1) > 1 && t->stride(1) != 1))
+                a.plain = false;
+            else {
+                table.p = t->data_ptr();
+                table.dim = t->size(1);
+                table.stride = sequences > 1 ? t->stride(0) : table.dim;
+            }
+        }
+        const int32_t *lengths = (const int32_t *)a.vector(sequences, at::kInt);
+        int64_t words = 0;
+        o = *a.at;
+        if (o != Py_None) {
+            if (!a.plain || !THPVariable_CheckTypeExact(Py_TYPE(o)) || !THPVariable_Unpack(o).defined() || THPVariable_Unpack(o).dim() != 2) Py_RETURN_NONE;
+            words = THPVariable_Unpack(o).size(1);
+            if (words <= 0 || words > INT_MAX) Py_RETURN_NONE;
+        }
+        const uint64_t *tree = (const uint64_t *)a.vector(q.rows * words, at::kLong, true);
+        const float scale = a.real();
+        const Args::Heads out = a.heads(&q);
+        size_t size;
+        void *ws = a.bytes(size), *stream = a.stream();
+        if (kc.heads != vc.heads || kc.pages != vc.pages || kc.page != vc.page) a.plain = false;
+        return call(a, [=] {
+            return f_attention_cache(q.p, q.row, q.head, (dsq_dtype)Args::dtype(q.type), (int)q.rows, (int)q.heads, (int)kc.heads, (int)q.dim,
+                                     starts, (int)sequences, max_rows, kc.p, vc.p, kc.pages, (int)kc.page, (const int32_t *)table.p,
+                                     table.stride, (int)table.dim, lengths, tree, (int)words, scale, out.p, out.row, out.head, ws, size, stream);
+        });
+    });
+}
+
+// init_heads(addresses of the calls for heads, in the order below)
+PyObject *init_heads(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "init_heads(five addresses)");
+        return nullptr;
+    }
+    void *p[5];
+    for (int i = 0; i < 5; ++i) {
+        p[i] = PyLong_AsVoidPtr(args[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    f_qk_norm_rope = (decltype(f_qk_norm_rope))p[0];
+    f_qk_norm_rope_bwd = (decltype(f_qk_norm_rope_bwd))p[1];
+    f_attention = (decltype(f_attention))p[2];
+    f_attention_bwd = (decltype(f_attention_bwd))p[3];
+    f_attention_cache = (decltype(f_attention_cache))p[4];
+    Py_RETURN_NONE;
+}
+
 // init_lm(addresses of the calls for language-model layers and their size queries, in the order below)
 PyObject *init_lm(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -445,7 +690,8 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(init), METHOD(quantize_act), METHOD(conv2d), METHOD(conv2d_requant), METHOD(conv2d_wq),
                          METHOD(soft_quantize_fwd), METHOD(soft_quantize_bwd), METHOD(init_lm), METHOD(rms_norm),
-                         METHOD(rms_norm_bwd), METHOD(linear_w4), METHOD(linear_w4a8), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(rms_norm_bwd), METHOD(linear_w4), METHOD(linear_w4a8), METHOD(init_heads), METHOD(qk_norm_rope),
+                         METHOD(qk_norm_rope_bwd), METHOD(attention), METHOD(attention_bwd), METHOD(attention_cache), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
