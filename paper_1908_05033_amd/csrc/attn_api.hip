@@ -39,6 +39,8 @@ int bits_of(int page)
     return -1;
 }
 
+size_t delta_bytes(int q_rows, int q_heads) { return ((size_t)q_rows * q_heads * 4 + 255) / 256 * 256; }
+
 #define TRY(call)                                                                                                        \
     if (const dsq_status status_ = (call)) return status_
 
@@ -77,7 +79,7 @@ size_t dsq_qk_norm_rope_bwd_bytes(int rows, int q_heads, int kv_heads, int dim)
 size_t dsq_attention_bwd_bytes(int q_rows, int q_heads)
 {
     if (q_rows <= 0 || q_rows > kMaxRows || q_heads <= 0 || q_heads > kMaxHeads) return 0;
-    return (size_t)q_rows * q_heads * 4;
+    return delta_bytes(q_rows, q_heads) + dsq_attn_bwd_partial_bytes(q_rows, q_heads);
 }
 
 size_t dsq_attention_cache_bytes(int sequences, int max_rows, int q_heads, int kv_heads, int dim)
@@ -243,7 +245,10 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
     a.q = {q, q_row, q_head}; a.k = {k, k_row, k_head}; a.v = {v, v_row, v_head}; a.out = {out, out_row, out_head};
     a.grad_out = {grad_out, grad_out_row, grad_out_head}; a.grad_q = {grad_q, grad_q_row, grad_q_head};
     a.grad_k = {grad_k, grad_k_row, grad_k_head}; a.grad_v = {grad_v, grad_v_row, grad_v_head};
-    a.lse = lse; a.delta = (float *)workspace; a.q_starts = q_starts; a.k_starts = k_starts ? k_starts : q_starts;
+    a.lse = lse; a.delta = (float *)workspace;
+    a.partial = (float *)((char *)workspace + (q_rows ? delta_bytes(q_rows, q_heads) : 0));
+    a.partial_bytes = q_rows ? dsq_attn_bwd_partial_bytes(q_rows, q_heads) : 0;
+    a.q_starts = q_starts; a.k_starts = k_starts ? k_starts : q_starts;
     a.q_rows = q_rows; a.k_rows = k_rows; a.q_heads = q_heads; a.kv_heads = kv_heads; a.dim = dim;
     a.sequences = sequences; a.causal = causal != 0; a.scale = scale;
     return of_hip(dsq_launch_attention_bwd(a, dtype, (hipStream_t)hip_stream));

@@ -7,6 +7,8 @@
 // time.  One owns rows of queries (D and dq), the other keys, over all heads that share them (dk and dv).  In both a
 // lane holds a column of the 32x32 results, so probabilities and ds are the second operand of the next product as they lie
 // in registers (attn_device.h).
+#include <type_traits>
+
 #include "attn_device.h"
 
 namespace {
@@ -21,14 +23,6 @@ template <class E>
 constexpr float kDrop = 1.0f;
 template <>
 constexpr float kDrop<_Float16> = 0x1p-10f;
-
-__device__ __forceinline__ v16f zeros()
-{
-    v16f z;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-    return z;
-}
 
 // Four consecutive elements a store: a lane's column of transposed 32x32 results as a row of the output.
 template <class E, int DT>
@@ -46,41 +40,21 @@ __device__ __forceinline__ void store_row(E *to, const v16f (&o)[DT], float by, 
         }
 }
 
-template <class E, int HD, int ROWS>
-struct Mover {
-    typedef Tile<E, HD> T;
-    static constexpr int PIECES = ROWS * HD * (int)sizeof(E) / 16 / 256;     // 16-byte pieces of a tile a thread moves
-    v4u at[PIECES];
-    // rows first .. first + ROWS - 1 of `p`, zeros from `end` on
-    __device__ __forceinline__ void fetch(const E *p, int64_t stride, int first, int end, int dim)
-    {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int piece = threadIdx.x + 256 * i, j = first + piece / T::UNITS, u = piece % T::UNITS;
-            at[i] = j < end && u * T::PER < dim ? *reinterpret_cast<const v4u *>(p + j * stride + u * T::PER) : v4u{0, 0, 0, 0};
-        }
-    }
-    __device__ __forceinline__ void put(E *t) const
-    {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int piece = threadIdx.x + 256 * i;
-            *reinterpret_cast<v4u *>(t + T::place(piece / T::UNITS, piece % T::UNITS)) = at[i];
-        }
-    }
-};
-
 // ---- queries ------------------------------------------------------------------------------------
+//
+// ROW_WAVES waves own 32 rows each; the others take other blocks of 32 keys for the same rows, and their sums are joined.
 
-template <class E, int HD>
-__global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_bwd_q_kernel(DsqAttnBwdArgs a, int tiles)
+template <class E, int HD, int ROW_WAVES>
+__global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void attn_bwd_q_kernel(DsqAttnBwdArgs a, int tiles)
 {
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int ROWS = 128, KEYS = 32, STEPS = HD / 16, DT = HD / 32;
-    __shared__ __align__(16) E ks[2][KEYS * HD], vs[2][KEYS * HD];
+    constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KEYS = 32 * SPLIT, STEPS = HD / 16, DT = HD / 32, BUFFERS = SPLIT == 1 ? 2 : 1;
+    constexpr int TILE = KEYS * HD, JOIN = (SPLIT - 1) * ROW_WAVES * DT * 4096;
+    __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
+    E *const tiles_at = reinterpret_cast<E *>(room);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5, part = wave / ROW_WAVES;
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
@@ -91,7 +65,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     const int last = s.at + ROWS < s.q_len ? s.at + ROWS - 1 : s.q_len - 1;
     const int k_end = visible(s, a.causal, last), count = (k_end + KEYS - 1) / KEYS;
 
-    const int row = s.at + wave * 32 + r;
+    const int first_row = s.at + wave % ROW_WAVES * 32, row = first_row + r;
     const bool there = row < s.q_len;
     const int64_t token = s.q0 + row;
     const E *qp = (const E *)a.q.p + token * a.q.row + head * a.q.head, *gp = (const E *)a.grad_out.p + token * a.grad_out.row + head * a.grad_out.head;
@@ -108,11 +82,11 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     }
     delta = both_sum(delta);
     const int64_t stat = (int64_t)head * a.q_rows + token;
-    if (there && h == 0) a.delta[stat] = delta;
+    if (there && h == 0 && part == 0) a.delta[stat] = delta;
     const int seen = there ? visible(s, a.causal, row) : 0;
     const float lse = seen > 0 ? a.lse[stat] * kLog2e - kLift<E> : 0.0f;
     delta *= kDrop<E>;
-    const int first_row = s.at + wave * 32, last_row = first_row + 31 < s.q_len ? first_row + 31 : s.q_len - 1;
+    const int last_row = first_row + 31 < s.q_len ? first_row + 31 : s.q_len - 1;
     const int whole = first_row + 31 < s.q_len ? visible(s, a.causal, first_row) : 0;
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
     const float c = a.scale * kLog2e;
@@ -124,169 +98,232 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     if (count > 0) {
         km.fetch(kp, a.k.row, 0, k_end, a.dim);
         vm.fetch(vp, a.v.row, 0, k_end, a.dim);
-        km.put(ks[0]);
-        vm.put(vs[0]);
-        __syncthreads();
     }
     for (int t = 0; t < count; ++t) {
-        const E *kt = ks[t & 1], *vt = vs[t & 1];
+        E *const kt = tiles_at + (BUFFERS == 2 ? t & 1 : 0) * 2 * TILE, *const vt = kt + TILE;
+        if (BUFFERS == 1) __syncthreads();
+        km.put(kt);
+        vm.put(vt);
+        __syncthreads();
         if (t + 1 < count) {
             km.fetch(kp, a.k.row, (t + 1) * KEYS, k_end, a.dim);
             vm.fetch(vp, a.v.row, (t + 1) * KEYS, k_end, a.dim);
         }
-        if (t * KEYS < any) {
+        const int at = t * KEYS + part * 32;                     // the wave's first key
+        if (at < any) {
             v16f x = zeros(), y = zeros();
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::row_operand(kt, r, i, h), q[i], x);
+            for (int i = 0; i < STEPS; ++i) x = multiply(T::row_operand(kt, part * 32 + r, i, h), q[i], x);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) y = multiply(T::row_operand(vt, r, i, h), g[i], y);
-            const bool masked = (t + 1) * KEYS > whole;
+            for (int i = 0; i < STEPS; ++i) y = multiply(T::row_operand(vt, part * 32 + r, i, h), g[i], y);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse));
                 x[i] = p * __builtin_fmaf(y[i], kDrop<E>, -delta);
             }
-            if (masked) {
+            if (at + 32 > whole) {
+                stay_a_branch();
+                const int left = seen - at - 4 * h;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = t * KEYS + 8 * (i / 4) + 4 * h + i % 4 < seen ? x[i] : 0.0f;
+                for (int i = 0; i < 16; ++i) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const V8 ds = operand_of<E>(x, half);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) dq[d] = multiply(T::column_operand(kt, half * 16, d * 32, lane), ds, dq[d]);
+                for (int d = 0; d < DT; ++d) dq[d] = multiply(T::column_operand(kt, part * 32 + half * 16, d * 32, lane), ds, dq[d]);
             }
         }
-        if (t + 1 < count) {
-            km.put(ks[(t + 1) & 1]);
-            vm.put(vs[(t + 1) & 1]);
-        }
-        __syncthreads();
     }
-    if (there) store_row<E, DT>((E *)a.grad_q.p + token * a.grad_q.row + head * a.grad_q.head, dq, a.scale, h, a.dim);
+    join<DT>(dq, reinterpret_cast<float *>(room), wave % ROW_WAVES, ROW_WAVES, part, SPLIT, lane);
+    if (there && part == 0) store_row<E, DT>((E *)a.grad_q.p + token * a.grad_q.row + head * a.grad_q.head, dq, a.scale, h, a.dim);
 }
 
 // ---- keys and values ------------------------------------------------------------------------------
+//
+// Two waves share 32 keys and blocks of 32 rows: one sums dv, the other dk.  Both form the scores, which costs a quarter more products
+// than one wave would need, but a wave that held both sums and both operands would have a SIMD to itself: so each has another at its
+// side, whose products run under its exponentials.  A workgroup has KEY_PAIRS such pairs side by side along the keys and
+// ROW_PAIRS along the rows, whose sums are joined at the end.  Where there are few keys the rows are split over workgroups too, which
+// leave their sums in the workspace for a kernel that adds them in order.
 
-template <class E, int HD>
-__global__ __launch_bounds__(256, 1) void attn_bwd_k_kernel(DsqAttnBwdArgs a, int tiles)
+template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS>
+__global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS == 4 ? 2 : 1) void attn_bwd_k_kernel(DsqAttnBwdArgs a, int tiles, int splits)
 {
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int KEYS = 128, ROWS = 32, STEPS = HD / 16, DT = HD / 32;
-    __shared__ __align__(16) E qs[2][ROWS * HD], gs[2][ROWS * HD];
-    __shared__ __align__(16) float stats[2][2][ROWS];
+    constexpr int PAIRS = KEY_PAIRS * ROW_PAIRS, THREADS = 128 * PAIRS, KEYS = 32 * KEY_PAIRS, ROWS = 32 * ROW_PAIRS;
+    constexpr int STEPS = HD / 16, DT = HD / 32, TILE = ROWS * HD, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
+    constexpr int BUFFERS = 4 * TILE * (int)sizeof(E) <= 65536 ? 2 : 1;
+    __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
+    __shared__ __align__(16) float stats[BUFFERS][2][ROWS];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
-    const int of = blockIdx.x / a.kv_heads, kv = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
-    // (the first keys of a causal prompt are seen by the most rows: they go first)
-    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, true, KEYS, of);
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
+    const int pair = wave % PAIRS, part = pair / KEY_PAIRS, group = a.q_heads / a.kv_heads;
+    const bool values = wave < PAIRS;                            // sums dv, not dk
+    // Workgroups go to the eight dies in turn: each die takes tiles side by side, which read the same rows.  (The first keys of a causal
+    // prompt are seen by the most rows: they go first.)
+    const int number = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, split = number / tiles % splits, kv = number / tiles / splits;
+    if (kv >= a.kv_heads) return;
+    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, true, KEYS, number % tiles);
     if (s.at < 0) return;
 
-    const int key = s.at + wave * 32 + r;
+    const int first_key = s.at + pair % KEY_PAIRS * 32, key = first_key + r;
     const bool there = key < s.k_len;
     const int64_t token = s.k0 + key;
-    const E *kp = (const E *)a.k.p + token * a.k.row + kv * a.k.head, *vp = (const E *)a.v.p + token * a.v.row + kv * a.v.head;
     V8 k[STEPS], v[STEPS];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-        k[i] = load_unit8(kp, 2 * i + h, a.dim, there);
-        v[i] = load_unit8(vp, 2 * i + h, a.dim, there);
+        k[i] = load_unit8((const E *)a.k.p + token * a.k.row + kv * a.k.head, 2 * i + h, a.dim, there);
+        v[i] = load_unit8((const E *)a.v.p + token * a.v.row + kv * a.v.head, 2 * i + h, a.dim, there && !values);
     }
-    // Row i sees keys up to i + off; rows from `first` on see one of the workgroup's, rows from `all` on every one of the wave's.
+    // Row i sees keys up to i + off; rows from `first` on see one of the workgroup's, and rows from `all` on every one of the wave's.
     const int off = s.k_len - s.q_len;
-    const int first = a.causal && s.at - off > 0 ? s.at - off : 0, t0 = first / ROWS;
-    const int count = s.q_len > t0 * ROWS ? (s.q_len + ROWS - 1) / ROWS - t0 : 0, turns = count * group;
-    const int wave_first = a.causal ? s.at + wave * 32 - off : 0, all = a.causal ? wave_first + 31 : 0;
+    const int first = a.causal && s.at - off > 0 ? (s.at - off) / 32 * 32 : 0;
+    const int all = a.causal ? first_key - off + 31 : 0;
     const float c = a.scale * kLog2e;
 
-    Mover<E, HD, ROWS> qm, gm;
+    Mover<E, HD, ROWS, THREADS> qm, gm;
     float stat = 0.0f;
-    auto fetch = [&](int n) {
-        const int head = kv * group + n / count, at = (t0 + n % count) * ROWS;
+    auto fetch = [&](int head, int at) {
         qm.fetch((const E *)a.q.p + s.q0 * a.q.row + head * a.q.head, a.q.row, at, s.q_len, a.dim);
         gm.fetch((const E *)a.grad_out.p + s.q0 * a.grad_out.row + head * a.grad_out.head, a.grad_out.row, at, s.q_len, a.dim);
         if (tid < 2 * ROWS) {
             const int row = at + tid % ROWS;
-            const int64_t i = (int64_t)head * a.q_rows + s.q0 + row;
-            // (rows that are not there see nothing)
-            if (tid < ROWS) stat = row < s.q_len ? a.lse[i] * kLog2e - kLift<E> : 0.0f;
-            else stat = row < s.q_len ? a.delta[i] * kDrop<E> : 0.0f;
+            const float *numbers = (tid < ROWS ? a.lse : a.delta) + (int64_t)head * a.q_rows + s.q0;
+            stat = row < s.q_len ? numbers[row] : 0.0f;
         }
-    };
-    auto put = [&](int b) {
-        qm.put(qs[b]);
-        gm.put(gs[b]);
-        if (tid < 2 * ROWS) stats[b][tid / ROWS][tid % ROWS] = stat;
     };
 
-    v16f dk[DT], dv[DT];
+    v16f sum[DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) dk[d] = zeros(), dv[d] = zeros();
-    if (turns > 0) {
-        fetch(0);
-        put(0);
-        __syncthreads();
-    }
-    for (int n = 0; n < turns; ++n) {
-        const E *qt = qs[n & 1], *gt = gs[n & 1];
-        const int at = (t0 + n % count) * ROWS;
-        if (n + 1 < turns) fetch(n + 1);
-        if (at + ROWS > wave_first) {
+    for (int d = 0; d < DT; ++d) sum[d] = zeros();
+    // blocks of rows, head by head
+    const int blocks = first < s.q_len ? (s.q_len - first + ROWS - 1) / ROWS : 0, from = (int)((int64_t)blocks * group * split / splits);
+    const auto walk = [&](auto role) {
+        constexpr bool VALUES = decltype(role)::value;
+        int left = (int)((int64_t)blocks * group * (split + 1) / splits) - from, b = 0;
+        int head = blocks ? kv * group + from / blocks : 0, at = blocks ? first + from % blocks * ROWS : 0;
+        if (BUFFERS == 2 && left > 0) fetch(head, at);
+        for (; left > 0; --left) {
+            E *const qt = reinterpret_cast<E *>(room) + b * 2 * TILE, *const gt = qt + TILE;
+            if (BUFFERS == 1) {
+                __syncthreads();
+                fetch(head, at);
+            }
+            qm.put(qt);
+            gm.put(gt);
+            if (tid < 2 * ROWS) stats[b][tid / ROWS][tid % ROWS] = tid < ROWS ? __builtin_fmaf(stat, kLog2e, -kLift<E>) : stat * kDrop<E>;
+            __syncthreads();
+            const int row = at + part * 32;                      // the wave's first row
+            at += ROWS;
+            if (at >= s.q_len) at = first, ++head;
+            if (BUFFERS == 2 && left > 1) fetch(head, at);
             v16f x = zeros(), y = zeros();
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::row_operand(qt, r, i, h), k[i], x);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) y = multiply(T::row_operand(gt, r, i, h), v[i], y);
-            const bool masked = at < all || at + ROWS > s.q_len;
+            for (int i = 0; i < STEPS; ++i) {
+                x = multiply(T::row_operand(qt, part * 32 + r, i, h), k[i], x);
+                if (!VALUES) y = multiply(T::row_operand(gt, part * 32 + r, i, h), v[i], y);
+            }
+            if (sizeof(E) == 2) ahead<(VALUES ? 1 : 2) * STEPS, (VALUES ? 1 : 2) * STEPS, STEPS>();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const v4f lse = *reinterpret_cast<const v4f *>(&stats[n & 1][0][8 * j + 4 * h]);
-                const v4f delta = *reinterpret_cast<const v4f *>(&stats[n & 1][1][8 * j + 4 * h]);
+                const v4f lse = *reinterpret_cast<const v4f *>(&stats[b][0][part * 32 + 8 * j + 4 * h]);
+                v4f delta = {};
+                if (!VALUES) delta = *reinterpret_cast<const v4f *>(&stats[b][1][part * 32 + 8 * j + 4 * h]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int i = 4 * j + e, row = at + 8 * j + 4 * h + e;
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse[e]));
-                    float ds = p * __builtin_fmaf(y[i], kDrop<E>, -delta[e]);
-                    if (masked) {
-                        const bool sees = row < s.q_len && (!a.causal || key <= row + off);
-                        p = sees ? p : 0.0f;
-                        ds = sees ? ds : 0.0f;
-                    }
-                    x[i] = p;
-                    y[i] = ds;
+                    const int i = 4 * j + e;
+                    x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse[e]));
+                    if (!VALUES) x[i] *= __builtin_fmaf(y[i], kDrop<E>, -delta[e]);
                 }
             }
+            if (row < all || row + 32 > s.q_len) {
+                stay_a_branch();
+                // rows from `seeing` on, up to the last, see the lane's key
+                const int seeing = (a.causal ? key - off : 0) - row - 4 * h, last = s.q_len - row - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = ((8 * (i / 4) + i % 4 >= seeing) & (8 * (i / 4) + i % 4 < last)) ? x[i] : 0.0f;
+            }
+            const E *columns = VALUES ? gt : qt;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const V8 p = operand_of<E>(x, half), ds = operand_of<E>(y, half);
+                const V8 w = operand_of<E>(x, half);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    dv[d] = multiply(T::column_operand(gt, half * 16, d * 32, lane), p, dv[d]);
-                    dk[d] = multiply(T::column_operand(qt, half * 16, d * 32, lane), ds, dk[d]);
-                }
+                for (int d = 0; d < DT; ++d) sum[d] = multiply(T::column_operand(columns, part * 32 + half * 16, d * 32, lane), w, sum[d]);
             }
+            if (sizeof(E) == 2) ahead<4 * DT, 2 * DT, 2 * DT>();
+            if (BUFFERS == 2) b ^= 1;
         }
-        if (n + 1 < turns) put((n + 1) & 1);
-        __syncthreads();
+    };
+    if (values) walk(std::true_type());
+    else walk(std::false_type());
+    join<DT>(sum, reinterpret_cast<float *>(room), wave / PAIRS * KEY_PAIRS + pair % KEY_PAIRS, 2 * KEY_PAIRS, part, ROW_PAIRS, lane);
+    if (!there || part > 0) return;
+    if (splits == 1) {
+        const DsqHeadsOut out = values ? a.grad_v : a.grad_k;
+        store_row<E, DT>((E *)out.p + token * out.row + kv * out.head, sum, values ? kDrop<E> : a.scale, h, a.dim);
+    } else {
+        store_row<float, DT>(a.partial + (((int64_t)split * 2 + (values ? 1 : 0)) * a.k_rows * a.kv_heads + token * a.kv_heads + kv) * a.dim, sum, 1.0f, h, a.dim);
     }
-    if (there) {
-        store_row<E, DT>((E *)a.grad_k.p + token * a.grad_k.row + kv * a.grad_k.head, dk, a.scale, h, a.dim);
-        store_row<E, DT>((E *)a.grad_v.p + token * a.grad_v.row + kv * a.grad_v.head, dv, kDrop<E>, h, a.dim);
+}
+
+// The sums of the splits, four elements of a head a thread.
+template <class E>
+__global__ __launch_bounds__(256) void attn_bwd_join_kernel(DsqAttnBwdArgs a, int splits)
+{
+    const int64_t each = (int64_t)a.k_rows * a.kv_heads * a.dim, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= each) return;
+    const int d = (int)(i % a.dim), kv = (int)(i / a.dim % a.kv_heads), token = (int)(i / a.dim / a.kv_heads);
+    if (a.k_starts && (token < a.k_starts[0] || token >= a.k_starts[a.sequences])) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const v4f *>(a.partial + (2 * s + which) * each + i);
+        const DsqHeadsOut out = which ? a.grad_v : a.grad_k;
+        const float by = which ? kDrop<E> : a.scale;
+        Side<E, 4> v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.at[e] = (E)(sum[e] * by);
+        store_side((E *)out.p + token * out.row + kv * out.head + d, v);
     }
+}
+
+constexpr int64_t kFew = 256 * 128;
+
+int tiles_of(const DsqAttnBwdArgs &a, int rows, int tile) { return a.q_starts ? rows / tile + a.sequences : (rows + tile - 1) / tile; }
+
+template <class E, int HD, int ROW_WAVES>
+hipError_t queries(const DsqAttnBwdArgs &a, hipStream_t stream)
+{
+    const int tiles = tiles_of(a, a.q_rows, 32 * ROW_WAVES);
+    attn_bwd_q_kernel<E, HD, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    return hipGetLastError();
+}
+template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS>
+hipError_t keys(const DsqAttnBwdArgs &a, hipStream_t stream)
+{
+    const int tiles = tiles_of(a, a.k_rows, 32 * KEY_PAIRS);
+    const int64_t groups = (int64_t)tiles * a.kv_heads, each = (int64_t)a.k_rows * a.kv_heads * a.dim;
+    // Workgroups for two rounds of the card, as far as there are rows and room.
+    int64_t splits = 512 / groups;
+    const int64_t blocks = (a.q_rows / (32 * ROW_PAIRS) + 1LL) * (a.q_heads / a.kv_heads), room = (int64_t)(a.partial_bytes / 8) / each;
+    for (const int64_t limit : {blocks, room, (int64_t)16}) splits = splits < limit ? splits : limit;
+    splits = splits < 1 ? 1 : splits;
+    attn_bwd_k_kernel<E, HD, KEY_PAIRS, ROW_PAIRS>
+        <<<(unsigned)((groups * splits + 7) / 8 * 8), 128 * KEY_PAIRS * ROW_PAIRS, 0, stream>>>(a, tiles, (int)splits);
+    if (const hipError_t e = hipGetLastError()) return e;
+    if (splits > 1) attn_bwd_join_kernel<E><<<(unsigned)((each / 4 + 255) / 256), 256, 0, stream>>>(a, (int)splits);
+    return hipGetLastError();
 }
 
 template <class E, int HD>
 hipError_t launch(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
-    const auto tiles = [&](int rows) { return a.q_starts ? rows / 128 + a.sequences : (rows + 127) / 128; };
-    const int tq = tiles(a.q_rows), tk = tiles(a.k_rows);
-    if (a.q_rows > 0) {
-        attn_bwd_q_kernel<E, HD><<<(unsigned)((int64_t)tq * a.q_heads), 256, 0, stream>>>(a, tq);
-        if (const hipError_t e = hipGetLastError()) return e;
-    }
-    if (a.k_rows > 0) attn_bwd_k_kernel<E, HD><<<(unsigned)((int64_t)tk * a.kv_heads), 256, 0, stream>>>(a, tk);
-    return hipGetLastError();
+    constexpr bool SINGLE = sizeof(E) == 4;
+    if (a.q_rows > 0)
+        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew ? queries<E, HD, 1>(a, stream) : queries<E, HD, SINGLE ? 2 : 4>(a, stream)) return e;
+    return a.k_rows > 0 ? keys<E, HD, SINGLE ? 1 : 2, 2>(a, stream) : hipSuccess;
 }
 
 template <class E>
@@ -296,6 +333,13 @@ hipError_t of_dim(const DsqAttnBwdArgs &a, hipStream_t stream)
 }
 
 }  // namespace
+
+// Eight times a binary32 dk and dv of as many keys as there are rows, at most 32 MB: 512 workgroups' worth.
+size_t dsq_attn_bwd_partial_bytes(int q_rows, int q_heads)
+{
+    const size_t all = (size_t)q_rows * q_heads * 8192;
+    return all < (32u << 20) ? all : 32u << 20;
+}
 
 hipError_t dsq_launch_attention_bwd(const DsqAttnBwdArgs &a, int type, hipStream_t stream)
 {

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel
     __shared__ float stat[4][2][32];
     __shared__ uint32_t seen_by[4][32];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
     const int per = row_tiles * a.kv_heads, number = blockIdx.x / per;
     const int kv = blockIdx.x % per % a.kv_heads, rt = blockIdx.x % per / a.kv_heads;
     const int group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
@@ -299,7 +299,7 @@ template <class E>
 __global__ __launch_bounds__(256) void attn_cache_join_kernel(DsqAttnCacheArgs a, int slots)
 {
     __shared__ float part[4][128], tops[4], sums[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_number();
     const int t = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads, group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
     int s = t;
     if (a.q_starts) {

@@ -98,6 +98,90 @@ __device__ __forceinline__ void wave_order()
     __builtin_amdgcn_wave_barrier();
 }
 
+// Rows of a tile on their way from memory to LDS: 16 bytes at a time, side by side in a row for lanes side by side.
+template <class E, int HD, int ROWS, int THREADS = 256>
+struct Mover {
+    typedef Tile<E, HD> T;
+    static constexpr int PIECES = ROWS * T::UNITS / THREADS, STEP = THREADS / T::UNITS;
+    v4u at[PIECES];
+    // Rows first .. first + ROWS - 1 of `p`; the last before `end` again from there on (what they are worth, the caller leaves out), and
+    // the first unit again past the elements of a head (their products meet zeros or are not stored): no load is behind a branch.
+    __device__ __forceinline__ void fetch(const E *p, int64_t stride, int first, int end, int dim)
+    {
+        const int u = threadIdx.x % T::UNITS, j = first + (int)(threadIdx.x / T::UNITS);
+        const E *from = p + (u * T::PER < dim ? u * T::PER : 0);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int row = j + STEP * i < end ? j + STEP * i : end - 1;
+            at[i] = *reinterpret_cast<const v4u *>(from + row * stride);
+        }
+    }
+    __device__ __forceinline__ void put(E *t) const
+    {
+        const int u = threadIdx.x % T::UNITS, row = threadIdx.x / T::UNITS;
+        E *const to = t + T::place(row, u);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            // (the exchange of units goes by the row's number modulo 16)
+            *reinterpret_cast<v4u *>(STEP % 16 == 0 ? to + STEP * i * HD : t + T::place(row + STEP * i, u)) = at[i];
+    }
+};
+
+// Keeps the compiler from computing a rarely taken branch's selections always.
+__device__ __forceinline__ void stay_a_branch() { asm volatile(""); }
+
+// The wave's number within its workgroup, known to the compiler to be the same for all lanes.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// Schedule of the products just written: FIRST of their READS loads from LDS before the first of MANY products, the others one after each, so
+// that a product does not wait for its own load.
+template <int READS, int MANY, int FIRST>
+__device__ __forceinline__ void ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+    constexpr int EACH = (READS - FIRST + MANY - 1) / MANY;
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (EACH > 0 && FIRST + i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    }
+}
+
+__device__ __forceinline__ v16f zeros()
+{
+    v16f z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
+// Adds up what `parts` waves hold, in their order: wave w of them leaves its numbers in LDS, the first adds and keeps the sum.
+// All waves of the workgroup take part; `of` numbers the groups of waves, `part` the wave within its group.
+template <int DT>
+__device__ __forceinline__ void join(v16f (&o)[DT], float *room, int of, int groups, int part, int parts, int lane)
+{
+    if (parts == 1) return;
+    __syncthreads();
+    if (part > 0) {
+        float *mine = room + (int64_t)((part - 1) * groups + of) * DT * 1024 + lane;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine[(d * 16 + i) * 64] = o[d][i];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int p = 0; p < parts - 1; ++p) {
+        const float *its = room + (int64_t)(p * groups + of) * DT * 1024 + lane;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] += its[(d * 16 + i) * 64];
+    }
+}
+
+constexpr int most(int a, int b) { return a > b ? a : b; }
+
 // One number for both lanes of a column.
 __device__ __forceinline__ float both_max(float v)
 {

@@ -10,13 +10,16 @@
 
 namespace {
 
-template <class E, int HD>
+// ROW_WAVES waves own 32 rows each; the others take other blocks of keys for the same rows, and their sums are joined at the end.
+template <class E, int HD, int ROW_WAVES>
 struct Fwd {
-    static constexpr int ROWS = 128, KEYS = sizeof(E) == 2 ? 64 : 32;
-    static constexpr int STEPS = HD / 16, DT = HD / 32, KT = KEYS / 32;
-    static constexpr int PIECES = KEYS * HD * (int)sizeof(E) / 16 / 256;     // 16-byte pieces of a tile a thread moves
+    static constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 && sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT * SPLIT;
+    static constexpr int STEPS = HD / 16, DT = HD / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
+    static constexpr int BYTES = most(BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
     typedef Tile<E, HD> T;
 };
+
+constexpr int64_t kFew = 256 * 128;
 
 // Keys of one row of a packed prompt.
 template <class E>
@@ -30,16 +33,17 @@ struct PromptKeys {
     __device__ const E *value(int j) const { return v + j * v_row; }
 };
 
-template <class E, int HD>
-__global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_fwd_kernel(DsqAttnArgs a, int tiles)
+template <class E, int HD, int ROW_WAVES>
+__global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64) ? 2 : 1) void attn_fwd_kernel(DsqAttnArgs a, int tiles)
 {
-    typedef Fwd<E, HD> F;
+    typedef Fwd<E, HD, ROW_WAVES> F;
     typedef typename F::T T;
     typedef typename Operand<E>::type V8;
-    __shared__ __align__(16) E ks[2][F::KEYS * HD], vs[2][F::KEYS * HD];
+    __shared__ __align__(16) char room[F::BYTES];
+    __shared__ float stat[2][F::SPLIT][F::ROWS];
 
     // heads that share keys meet on one of the eight dies, which take workgroups in turn
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5, part = wave / ROW_WAVES;
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
@@ -51,7 +55,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     const int last = s.at + F::ROWS < s.q_len ? s.at + F::ROWS - 1 : s.q_len - 1;
     const int k_end = visible(s, a.causal, last), count = (k_end + F::KEYS - 1) / F::KEYS;
 
-    const int row = s.at + wave * 32 + r;                    // this lane's row
+    const int first_row = s.at + wave % ROW_WAVES * 32, row = first_row + r;     // this lane's row
     const bool there = row < s.q_len;
     const E *qp = (const E *)a.q.p + (int64_t)(s.q0 + row) * a.q.row + head * a.q.head;
     V8 q[F::STEPS];
@@ -59,60 +63,44 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     for (int i = 0; i < F::STEPS; ++i) q[i] = load_unit8(qp, 2 * i + h, a.dim, there);
     const int seen = there ? visible(s, a.causal, row) : 0;
     // keys that all of the wave's rows see, and that any does
-    const int first_row = s.at + wave * 32, last_row = first_row + 31 < s.q_len ? first_row + 31 : s.q_len - 1;
+    const int last_row = first_row + 31 < s.q_len ? first_row + 31 : s.q_len - 1;
     const int whole = first_row + 31 < s.q_len ? visible(s, a.causal, first_row) : 0;
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
 
-    v4u kr[F::PIECES], vr[F::PIECES];
+    Mover<E, HD, F::KEYS> km, vm;
     auto fetch = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < F::PIECES; ++i) {
-            const int piece = tid + 256 * i, j = t * F::KEYS + piece / T::UNITS, u = piece % T::UNITS;
-            const bool ok = j < k_end && u * T::PER < a.dim;
-            kr[i] = ok ? *reinterpret_cast<const v4u *>(kp + j * a.k.row + u * T::PER) : v4u{0, 0, 0, 0};
-            vr[i] = ok ? *reinterpret_cast<const v4u *>(vp + j * a.v.row + u * T::PER) : v4u{0, 0, 0, 0};
-        }
+        km.fetch(kp, a.k.row, t * F::KEYS, k_end, a.dim);
+        vm.fetch(vp, a.v.row, t * F::KEYS, k_end, a.dim);
     };
-    auto put = [&](int b) {
-#pragma unroll
-        for (int i = 0; i < F::PIECES; ++i) {
-            const int piece = tid + 256 * i, at = T::place(piece / T::UNITS, piece % T::UNITS);
-            *reinterpret_cast<v4u *>(ks[b] + at) = kr[i];
-            *reinterpret_cast<v4u *>(vs[b] + at) = vr[i];
-        }
-    };
-
     const float c = a.scale * kLog2e;
     float m = kNoKey, l = 0.0f;
     v16f o[F::DT];
 #pragma unroll
-    for (int d = 0; d < F::DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-
-    if (count > 0) {
-        fetch(0);
-        put(0);
-        __syncthreads();
-    }
+    for (int d = 0; d < F::DT; ++d) o[d] = zeros();
+    if (count > 0) fetch(0);
     for (int t = 0; t < count; ++t) {
-        const E *kt = ks[t & 1], *vt = vs[t & 1];
+        E *const kt = reinterpret_cast<E *>(room) + (F::BUFFERS == 2 ? t & 1 : 0) * 2 * F::TILE, *const vt = kt + F::TILE;
+        if (F::BUFFERS == 1) __syncthreads();
+        km.put(kt);
+        vm.put(vt);
+        __syncthreads();
         if (t + 1 < count) fetch(t + 1);
-        if (t * F::KEYS < any) {
+        const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
+        if (at < any) {
             v16f x[F::KT];
 #pragma unroll
             for (int n = 0; n < F::KT; ++n) {
+                x[n] = zeros();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[n][i] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < F::STEPS; ++i) x[n] = multiply(T::row_operand(kt, n * 32 + r, i, h), q[i], x[n]);
+                for (int i = 0; i < F::STEPS; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
             }
-            if ((t + 1) * F::KEYS > whole) {
+            if (at + 32 * F::KT > whole) {
+                stay_a_branch();
+                const int left = seen - at - 4 * h;
 #pragma unroll
                 for (int n = 0; n < F::KT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        x[n][i] = t * F::KEYS + n * 32 + 8 * (i / 4) + 4 * h + i % 4 < seen ? x[n][i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) x[n][i] = n * 32 + 8 * (i / 4) + i % 4 < left ? x[n][i] : -INFINITY;
             }
             float most = x[0][0];
 #pragma unroll
@@ -144,14 +132,34 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
                     const V8 p = operand_of<E>(x[n], half);
 #pragma unroll
                     for (int d = 0; d < F::DT; ++d)
-                        o[d] = multiply(T::column_operand(vt, n * 32 + half * 16, d * 32, lane), p, o[d]);
+                        o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
                 }
         }
-        if (t + 1 < count) put((t + 1) & 1);
-        __syncthreads();
     }
 
     l = both_sum(l);
+    if (F::SPLIT > 1) {
+        // the waves' sums to one reference, then together
+        const int mine = wave % ROW_WAVES * 32 + r;
+        if (h == 0) stat[0][part][mine] = m;
+        __syncthreads();
+        float top = m;
+#pragma unroll
+        for (int p = 0; p < F::SPLIT; ++p) top = __builtin_elementwise_maximum(top, stat[0][p][mine]);
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= f;
+        if (h == 0) stat[1][part][mine] = l;
+#pragma unroll
+        for (int d = 0; d < F::DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        join<F::DT>(o, reinterpret_cast<float *>(room), wave % ROW_WAVES, ROW_WAVES, part, F::SPLIT, lane);
+        if (part > 0) return;
+        l = 0.0f;
+#pragma unroll
+        for (int p = 0; p < F::SPLIT; ++p) l += stat[1][p][mine];
+    }
     const float inv = seen > 0 ? 1.0f / l : 0.0f;
     bool bad = false;
     E *op = (E *)a.out.p + (int64_t)(s.q0 + row) * a.out.row + head * a.out.head;
@@ -186,18 +194,24 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 || HD == 64 ? 2 : 1) void attn_
     }
 }
 
-template <class E, int HD>
+template <class E, int HD, int ROW_WAVES>
 hipError_t launch(const DsqAttnArgs &a, hipStream_t stream)
 {
-    const int tiles = a.q_starts ? a.q_rows / Fwd<E, HD>::ROWS + a.sequences : (a.q_rows + Fwd<E, HD>::ROWS - 1) / Fwd<E, HD>::ROWS;
-    attn_fwd_kernel<E, HD><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    const int rows = Fwd<E, HD, ROW_WAVES>::ROWS, tiles = a.q_starts ? a.q_rows / rows + a.sequences : (a.q_rows + rows - 1) / rows;
+    attn_fwd_kernel<E, HD, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
+}
+
+template <class E, int HD>
+hipError_t of_rows(const DsqAttnArgs &a, hipStream_t stream)
+{
+    return (int64_t)a.q_rows * a.q_heads < kFew ? launch<E, HD, 1>(a, stream) : launch<E, HD, 4>(a, stream);
 }
 
 template <class E>
 hipError_t of_dim(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? launch<E, 64>(a, stream) : launch<E, 128>(a, stream);
+    return a.dim <= 64 ? of_rows<E, 64>(a, stream) : of_rows<E, 128>(a, stream);
 }
 
 }  // namespace

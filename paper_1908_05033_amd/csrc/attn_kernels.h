@@ -64,10 +64,14 @@ struct DsqAttnBwdArgs {
     DsqHeadsOut grad_q, grad_k, grad_v;
     const float *lse;
     float *delta;                            // [q_heads][q_rows]: sums of out * grad_out
+    float *partial;                          // room for sums of dk and dv of parts of the rows
+    size_t partial_bytes;
     const int32_t *q_starts, *k_starts;
     int q_rows, k_rows, q_heads, kv_heads, dim, sequences, causal;
     float scale;
 };
+// Room that joins sums over parts of the rows where there are few keys.
+size_t dsq_attn_bwd_partial_bytes(int q_rows, int q_heads);
 hipError_t dsq_launch_attention_bwd(const DsqAttnBwdArgs &a, int type, hipStream_t stream);
 
 struct DsqAttnCacheArgs {
