@@ -265,7 +265,7 @@ dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head, dsq
     if (max_rows <= 0 || pages < 0 || table_pages < 0 || (!q_starts && rows != sequences) || (tree && tree_words <= 0)) return DSQ_ERR_SHAPE;
     if (max_rows > kMaxRows || pages > 0x7fffffff || bits < 0 || (int64_t)table_pages << bits > kMaxKeys) return DSQ_ERR_UNSUPPORTED;
     if (rows == 0 || sequences == 0) return DSQ_OK;
-    const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads);
+    const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads, sequences, (int64_t)table_pages << bits);
     if ((int64_t)(p.slots + sequences) * p.row_tiles * kv_heads > 0x7fffffff || (int64_t)rows * q_heads > 0x7fffffff ||
         (((int64_t)table_pages << bits) / 128 + 1) * sequences > 0x7fffffff)
         return DSQ_ERR_UNSUPPORTED;

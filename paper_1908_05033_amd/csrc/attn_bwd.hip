@@ -141,22 +141,27 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
 
 // ---- keys and values ------------------------------------------------------------------------------
 //
-// Two waves share 32 keys and blocks of 32 rows: one sums dv, the other dk.  Both form the scores, which costs a quarter more products
-// than one wave would need, but a wave that held both sums and both operands would have a SIMD to itself: so each has another at its
-// side, whose products run under its exponentials.  A workgroup has KEY_PAIRS such pairs side by side along the keys and
+// Two waves share 32 keys and blocks of 32 rows: one forms the scores and p and sums dv, the other forms grad_out . v and ds and sums dk,
+// with p handed over in LDS.  Each so holds one operand and one sum in registers, has SUB blocks of rows under way at once, and another
+// wave on its SIMD whose products run under its exponentials.  A workgroup has KEY_PAIRS such pairs side by side along the keys and
 // ROW_PAIRS along the rows, whose sums are joined at the end.  Where there are few keys the rows are split over workgroups too, which
 // leave their sums in the workspace for a kernel that adds them in order.
+//
+// (Measured beside it at 4 x 2048 rows, 16 heads of 128 in four groups: both waves form the scores and nothing is handed over 268 us for 224;
+// one wave holds both sums and operands, one wave a SIMD, 422; one block of rows at a time 234; pairs 2 x 1 or 1 x 2, two workgroups
+// a compute unit, 350 and 284.)
 
-template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS>
+template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS, int SUB>
 __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS == 4 ? 2 : 1) void attn_bwd_k_kernel(DsqAttnBwdArgs a, int tiles, int splits)
 {
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int PAIRS = KEY_PAIRS * ROW_PAIRS, THREADS = 128 * PAIRS, KEYS = 32 * KEY_PAIRS, ROWS = 32 * ROW_PAIRS;
+    constexpr int PAIRS = KEY_PAIRS * ROW_PAIRS, THREADS = 128 * PAIRS, KEYS = 32 * KEY_PAIRS, MINE = 32 * SUB, ROWS = MINE * ROW_PAIRS;
     constexpr int STEPS = HD / 16, DT = HD / 32, TILE = ROWS * HD, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
-    constexpr int BUFFERS = 4 * TILE * (int)sizeof(E) <= 65536 ? 2 : 1;
-    __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
-    __shared__ __align__(16) float stats[BUFFERS][2][ROWS];
+    __shared__ __align__(16) char room[most(2 * TILE * (int)sizeof(E), JOIN)];
+    __shared__ __align__(16) float handed[PAIRS][SUB][16 * 64], stats[2][ROWS];
+
+    E *const qt = reinterpret_cast<E *>(room), *const gt = qt + TILE;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
     const int pair = wave % PAIRS, part = pair / KEY_PAIRS, group = a.q_heads / a.kv_heads;
@@ -171,12 +176,11 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
     const int first_key = s.at + pair % KEY_PAIRS * 32, key = first_key + r;
     const bool there = key < s.k_len;
     const int64_t token = s.k0 + key;
-    V8 k[STEPS], v[STEPS];
+    const DsqHeads mine = values ? a.k : a.v;
+    const E *its = (const E *)mine.p + token * mine.row + kv * mine.head;
+    V8 own[STEPS];
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        k[i] = load_unit8((const E *)a.k.p + token * a.k.row + kv * a.k.head, 2 * i + h, a.dim, there);
-        v[i] = load_unit8((const E *)a.v.p + token * a.v.row + kv * a.v.head, 2 * i + h, a.dim, there && !values);
-    }
+    for (int i = 0; i < STEPS; ++i) own[i] = load_unit8(its, 2 * i + h, a.dim, there);
     // Row i sees keys up to i + off; rows from `first` on see one of the workgroup's, and rows from `all` on every one of the wave's.
     const int off = s.k_len - s.q_len;
     const int first = a.causal && s.at - off > 0 ? (s.at - off) / 32 * 32 : 0;
@@ -194,7 +198,6 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
             stat = row < s.q_len ? numbers[row] : 0.0f;
         }
     };
-
     v16f sum[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) sum[d] = zeros();
@@ -202,58 +205,72 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
     const int blocks = first < s.q_len ? (s.q_len - first + ROWS - 1) / ROWS : 0, from = (int)((int64_t)blocks * group * split / splits);
     const auto walk = [&](auto role) {
         constexpr bool VALUES = decltype(role)::value;
-        int left = (int)((int64_t)blocks * group * (split + 1) / splits) - from, b = 0;
+        int left = (int)((int64_t)blocks * group * (split + 1) / splits) - from;
         int head = blocks ? kv * group + from / blocks : 0, at = blocks ? first + from % blocks * ROWS : 0;
-        if (BUFFERS == 2 && left > 0) fetch(head, at);
+        if (left > 0) fetch(head, at);
+        v4f *const slot = reinterpret_cast<v4f *>(handed[pair][0]) + lane;
         for (; left > 0; --left) {
-            E *const qt = reinterpret_cast<E *>(room) + b * 2 * TILE, *const gt = qt + TILE;
-            if (BUFFERS == 1) {
-                __syncthreads();
-                fetch(head, at);
-            }
+            __syncthreads();
             qm.put(qt);
             gm.put(gt);
-            if (tid < 2 * ROWS) stats[b][tid / ROWS][tid % ROWS] = tid < ROWS ? __builtin_fmaf(stat, kLog2e, -kLift<E>) : stat * kDrop<E>;
+            if (tid < 2 * ROWS) stats[tid / ROWS][tid % ROWS] = tid < ROWS ? __builtin_fmaf(stat, kLog2e, -kLift<E>) : stat * kDrop<E>;
             __syncthreads();
-            const int row = at + part * 32;                      // the wave's first row
+            const int row0 = at + part * MINE;                      // the wave's first row
             at += ROWS;
             if (at >= s.q_len) at = first, ++head;
-            if (BUFFERS == 2 && left > 1) fetch(head, at);
-            v16f x = zeros(), y = zeros();
+            if (left > 1) fetch(head, at);
+            v16f x[SUB];
+            const E *rows = VALUES ? qt : gt;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                x = multiply(T::row_operand(qt, part * 32 + r, i, h), k[i], x);
-                if (!VALUES) y = multiply(T::row_operand(gt, part * 32 + r, i, h), v[i], y);
-            }
-            if (sizeof(E) == 2) ahead<(VALUES ? 1 : 2) * STEPS, (VALUES ? 1 : 2) * STEPS, STEPS>();
+            for (int u = 0; u < SUB; ++u) x[u] = zeros();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const v4f lse = *reinterpret_cast<const v4f *>(&stats[b][0][part * 32 + 8 * j + 4 * h]);
-                v4f delta = {};
-                if (!VALUES) delta = *reinterpret_cast<const v4f *>(&stats[b][1][part * 32 + 8 * j + 4 * h]);
+            for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 4 * j + e;
-                    x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse[e]));
-                    if (!VALUES) x[i] *= __builtin_fmaf(y[i], kDrop<E>, -delta[e]);
+                for (int u = 0; u < SUB; ++u) x[u] = multiply(T::row_operand(rows, part * MINE + u * 32 + r, i, h), own[i], x[u]);
+            if (sizeof(E) == 2) ahead<SUB * STEPS, SUB * STEPS, STEPS>();
+            if (VALUES) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    const int row = row0 + u * 32;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const v4f lse = *reinterpret_cast<const v4f *>(&stats[0][part * MINE + u * 32 + 8 * j + 4 * h]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[u][4 * j + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][4 * j + e], c, -lse[e]));
+                    }
+                    if (row < all || row + 32 > s.q_len) {
+                        stay_a_branch();
+                        // rows from `seeing` on, up to the last, see the lane's key
+                        const int seeing = (a.causal ? key - off : 0) - row - 4 * h, last = s.q_len - row - 4 * h;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[u][i] = ((8 * (i / 4) + i % 4 >= seeing) & (8 * (i / 4) + i % 4 < last)) ? x[u][i] : 0.0f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) slot[(u * 4 + j) * 64] = v4f{x[u][4 * j], x[u][4 * j + 1], x[u][4 * j + 2], x[u][4 * j + 3]};
                 }
             }
-            if (row < all || row + 32 > s.q_len) {
-                stay_a_branch();
-                // rows from `seeing` on, up to the last, see the lane's key
-                const int seeing = (a.causal ? key - off : 0) - row - 4 * h, last = s.q_len - row - 4 * h;
+            __syncthreads();
+            if (!VALUES) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = ((8 * (i / 4) + i % 4 >= seeing) & (8 * (i / 4) + i % 4 < last)) ? x[i] : 0.0f;
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const v4f delta = *reinterpret_cast<const v4f *>(&stats[1][part * MINE + u * 32 + 8 * j + 4 * h]), p = slot[(u * 4 + j) * 64];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[u][4 * j + e] = p[e] * __builtin_fmaf(x[u][4 * j + e], kDrop<E>, -delta[e]);
+                    }
             }
             const E *columns = VALUES ? gt : qt;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const V8 w = operand_of<E>(x, half);
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) sum[d] = multiply(T::column_operand(columns, part * 32 + half * 16, d * 32, lane), w, sum[d]);
-            }
-            if (sizeof(E) == 2) ahead<4 * DT, 2 * DT, 2 * DT>();
-            if (BUFFERS == 2) b ^= 1;
+                for (int half = 0; half < 2; ++half) {
+                    const V8 w = operand_of<E>(x[u], half);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+                        sum[d] = multiply(T::column_operand(columns, part * MINE + u * 32 + half * 16, d * 32, lane), w, sum[d]);
+                }
+            if (sizeof(E) == 2) ahead<SUB * 4 * DT, SUB * 2 * DT, 2 * DT>();
         }
     };
     if (values) walk(std::true_type());
@@ -300,17 +317,17 @@ hipError_t queries(const DsqAttnBwdArgs &a, hipStream_t stream)
     attn_bwd_q_kernel<E, HD, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
-template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS>
+template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS, int SUB>
 hipError_t keys(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     const int tiles = tiles_of(a, a.k_rows, 32 * KEY_PAIRS);
     const int64_t groups = (int64_t)tiles * a.kv_heads, each = (int64_t)a.k_rows * a.kv_heads * a.dim;
     // Workgroups for two rounds of the card, as far as there are rows and room.
     int64_t splits = 512 / groups;
-    const int64_t blocks = (a.q_rows / (32 * ROW_PAIRS) + 1LL) * (a.q_heads / a.kv_heads), room = (int64_t)(a.partial_bytes / 8) / each;
+    const int64_t blocks = (a.q_rows / (32 * SUB * ROW_PAIRS) + 1LL) * (a.q_heads / a.kv_heads), room = (int64_t)(a.partial_bytes / 8) / each;
     for (const int64_t limit : {blocks, room, (int64_t)16}) splits = splits < limit ? splits : limit;
     splits = splits < 1 ? 1 : splits;
-    attn_bwd_k_kernel<E, HD, KEY_PAIRS, ROW_PAIRS>
+    attn_bwd_k_kernel<E, HD, KEY_PAIRS, ROW_PAIRS, SUB>
         <<<(unsigned)((groups * splits + 7) / 8 * 8), 128 * KEY_PAIRS * ROW_PAIRS, 0, stream>>>(a, tiles, (int)splits);
     if (const hipError_t e = hipGetLastError()) return e;
     if (splits > 1) attn_bwd_join_kernel<E><<<(unsigned)((each / 4 + 255) / 256), 256, 0, stream>>>(a, (int)splits);
@@ -323,7 +340,7 @@ hipError_t launch(const DsqAttnBwdArgs &a, hipStream_t stream)
     constexpr bool SINGLE = sizeof(E) == 4;
     if (a.q_rows > 0)
         if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew ? queries<E, HD, 1>(a, stream) : queries<E, HD, SINGLE ? 2 : 4>(a, stream)) return e;
-    return a.k_rows > 0 ? keys<E, HD, SINGLE ? 1 : 2, 2>(a, stream) : hipSuccess;
+    return a.k_rows > 0 ? keys<E, HD, SINGLE ? 1 : 2, 2, 2>(a, stream) : hipSuccess;
 }
 
 template <class E>

@@ -1,22 +1,17 @@
 // Attention of single tokens, and of trees of drafted tokens, over a paged cache.
 //
-// The rows of a key head are the drafted tokens of a sequence times the query heads that share it; 32 of them are one tile.  A
-// sequence's keys are cut into chunks of one length for all sequences, so that a batch of many lengths fills the card evenly, and a
-// workgroup takes a chunk of a key head for a tile of rows: its four waves take blocks of 32 keys in turn, each with the running
-// maximum and sum of a softmax, and join in LDS.  A sequence of one chunk is finished there; the others leave normed rows
-// and the logarithms of their sums, which a second kernel joins.  Keys and values are read once for 32 rows, in whole rows of a page,
-// and go through LDS of the wave's own, so a wave waits for nothing but its own loads.
+// The rows of a key head are the drafted tokens of a sequence times the query heads that share it.  A sequence's keys are cut into
+// chunks of one length for all sequences, so that a batch of many lengths fills the card evenly, and a workgroup takes a chunk of a
+// key head.  Up to 32 rows are one tile: the waves take blocks of 32 keys in turn, each with the running maximum and sum of a
+// softmax, and join in LDS; a block goes through LDS of the wave's own, so a wave waits for nothing but its own loads.  Of
+// more rows each of four waves takes 32, over tiles of keys that they share.  A sequence of one chunk is finished there; the others
+// leave normed rows and the logarithms of their sums, which a second kernel joins.
 #include "attn_cache_plan.h"
 #include "attn_device.h"
 
 namespace {
 
 constexpr int kUnit = 128;                   // keys a chunk is a multiple of: a block for each wave
-
-struct Chunk {
-    int sequence, first, count, chunks;      // first: key; count: keys; chunks: of the sequence (0 without keys)
-    int length;
-};
 
 __device__ __forceinline__ int sum_to(int v, int lane)
 {
@@ -29,25 +24,27 @@ __device__ __forceinline__ int sum_to(int v, int lane)
 
 __device__ __forceinline__ int length_of(const DsqAttnCacheArgs &a, int s) { return clamped(a.lengths[s], a.table_pages << a.page_bits); }
 
-// Units of keys a chunk has: the same for all sequences.
-__device__ __forceinline__ int chunk_units(const DsqAttnCacheArgs &a, int slots, int lane)
-{
-    int total = 0;
-    for (int s = lane; s < a.sequences; s += 64) total += (length_of(a, s) + kUnit - 1) / kUnit;
-    for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
-    const int c = (total + slots - 1) / slots;
-    return c > 0 ? c : 1;
-}
-
-// Chunks are numbered as tiles of sequences are: sequence s has them from (units before it) / units a chunk + s on.  Either the chunk of
-// a number, or (`number` negative) the first number of sequence `s`; all 64 lanes take part.
-__device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int units, int number, int &s)
+// Chunks have the same number of units for all sequences, and are numbered as tiles of sequences are: sequence s has them from (units
+// before it) / units a chunk + s on.  Finds the sequence of chunk `number`, or (`number` negative) takes the sequence s; returns
+// its first number, and the units of a chunk.  All 64 lanes take part; s is negative if there is none.
+__device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int slots, int number, int &s, int &units)
 {
     const int lane = threadIdx.x & 63;
+    const auto units_of = [&](int i) { return i < a.sequences ? (length_of(a, i) + kUnit - 1) / kUnit : 0; };
+    const int head = units_of(lane), head_sum = sum_to(head, lane);      // (the first 64 are looked at once)
+    int total = __shfl(head_sum, 63);
+    if (a.sequences > 64) {
+        int more = 0;
+        for (int i = lane + 64; i < a.sequences; i += 64) more += units_of(i);
+        for (int off = 32; off > 0; off >>= 1) more += __shfl_xor(more, off);
+        total += more;
+    }
+    units = (total + slots - 1) / slots;
+    units = units > 0 ? units : 1;
     int before = 0, found = -1, at = -1;
     for (int base = 0; base < a.sequences; base += 64) {
-        const int i = base + lane, mine = i < a.sequences ? (length_of(a, i) + kUnit - 1) / kUnit : 0;
-        const int sum = sum_to(mine, lane), slot = (before + sum - mine) / units + i;
+        const int i = base + lane, mine = base ? units_of(i) : head, sum = base ? sum_to(mine, lane) : head_sum;
+        const int slot = (before + sum - mine) / units + i;
         const uint64_t ok = __ballot(i < a.sequences && (number < 0 ? i <= s : slot <= number));
         if (ok == 0) break;
         const int last = 63 - __clzll((long long)ok);
@@ -57,6 +54,7 @@ __device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int units,
         if (last < 63) break;
     }
     s = __builtin_amdgcn_readfirstlane(found);
+    units = __builtin_amdgcn_readfirstlane(units);
     return __builtin_amdgcn_readfirstlane(at);
 }
 
@@ -108,47 +106,114 @@ struct CacheKeys {
     __device__ const E *value(int j) const { return v + pages.row(first + j) * dim; }
 };
 
-template <class E, int HD>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel(DsqAttnCacheArgs a, int slots, int row_tiles)
+// What a workgroup has to do: a chunk of a sequence's keys for a key head.
+struct Work {
+    int s, first, end, length, tokens, mine, t0;   // keys first .. end - 1; rows: `mine` of its `tokens` from row t0 on
+    bool whole;                                    // the sequence has no other chunk
+    __device__ __forceinline__ void of_sequence(const DsqAttnCacheArgs &a)
+    {
+        length = length_of(a, s);
+        t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s;
+        tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
+        mine = tokens < a.max_rows ? tokens : a.max_rows;
+    }
+    // slots: chunks that all keys are cut into; none: a workgroup takes all keys of a sequence
+    __device__ __forceinline__ bool find(const DsqAttnCacheArgs &a, int slots, int number)
+    {
+        if (slots == 0) {
+            s = number;
+            of_sequence(a);
+            first = 0;
+            end = length;
+            whole = true;
+            return true;
+        }
+        int units;
+        const int slot0 = first_chunk(a, slots, number, s, units);
+        if (s < 0) return false;
+        const int chunk = units * kUnit;
+        of_sequence(a);
+        if ((int64_t)(number - slot0) * chunk >= length && number != slot0) return false;
+        first = (number - slot0) * chunk;
+        end = length - first < chunk ? length : first + chunk;
+        whole = length <= chunk;
+        return true;
+    }
+};
+
+// Where the logarithms of a row's chunks lie side by side, behind all rows: [kv heads][rows][chunks].
+__device__ __forceinline__ float *logs_of(const DsqAttnCacheArgs &a, int slots, int kv, int of)
+{
+    const int64_t most_rows = (int64_t)a.max_rows * (a.q_heads / a.kv_heads), chunks = slots + a.sequences;
+    return a.partial + chunks * a.kv_heads * most_rows * a.dim + (kv * most_rows + of) * chunks;
+}
+
+// A finished row (its logarithm to base 2, normed elements lane and lane + 64 of a wave): to the output, or to where chunks are joined.
+template <class E>
+__device__ __forceinline__ void leave_row(const DsqAttnCacheArgs &a, const Work &w, int slots, int number, int kv, int of, bool seen, float log2, const float y[2])
+{
+    const int lane = threadIdx.x & 63, group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
+    if (w.whole) {
+        E *to = (E *)a.out.p + (int64_t)(w.t0 + of / group) * a.out.row + (kv * group + of % group) * a.out.head;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (lane + 64 * e < a.dim) to[lane + 64 * e] = (E)y[e];
+        return;
+    }
+    // (a row whose scores are all -inf is NaN by the formula, but only where no other chunk has more)
+    if (!(log2 > kNoKey) && log2 == log2) log2 = kNoKey;
+    const int64_t place = ((int64_t)number * a.kv_heads + kv) * most_rows + of;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (lane + 64 * e < a.dim) a.partial[place * a.dim + lane + 64 * e] = y[e];
+    if (lane == 0) logs_of(a, slots, kv, of)[number] = seen ? log2 : -INFINITY;
+}
+
+template <class E>
+__device__ __forceinline__ float again(const DsqAttnCacheArgs &a, const Work &w, const Pages &pages, int kv, int of, float c, float y[2])
+{
+    const int group = a.q_heads / a.kv_heads, token = of / group;
+    const Tree its = {a.tree ? a.tree + (int64_t)(w.t0 + token) * a.tree_words : nullptr, a.tree_words, token, w.length - w.tokens};
+    const CacheKeys<E> keys = {(const E *)a.k_cache, (const E *)a.v_cache, pages, its, w.first, w.end - w.first, a.dim};
+    return row_again<E>((const E *)a.q.p + (int64_t)(w.t0 + token) * a.q.row + (kv * group + of % group) * a.q.head, a.dim, c, keys, y);
+}
+
+// Puts -inf in the place of the scores of 32 keys whose bit is not set.
+__device__ __forceinline__ void hide_keys(v16f &x, uint32_t mask, int h)
+{
+    if (!__any(mask != 0xffffffffu)) return;
+    stay_a_branch();
+    mask >>= 4 * h;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = mask >> (8 * (i / 4) + i % 4) & 1 ? x[i] : -INFINITY;
+}
+
+// ---- up to 32 rows: WAVES waves take blocks of 32 keys in turn ------------------------------------------
+
+template <class E, int HD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel(DsqAttnCacheArgs a, int slots)
 {
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int STEPS = HD / 16, DT = HD / 32, PIECES = 32 * T::UNITS / 64, PITCH = 33;
-    constexpr int WAVE_BYTES = HD * PITCH * 4 > 64 * HD * (int)sizeof(E) ? HD * PITCH * 4 : 64 * HD * (int)sizeof(E);
-    __shared__ __align__(16) char room[4 * WAVE_BYTES];
-    __shared__ float stat[4][2][32];
-    __shared__ uint32_t seen_by[4][32];
+    constexpr int STEPS = HD / 16, DT = HD / 32, PIECES = 32 * T::UNITS / 64, PITCH = 33, STRIDE = 32 * WAVES;
+    constexpr int WAVE_BYTES = most(HD * PITCH * 4, 64 * HD * (int)sizeof(E));
+    __shared__ __align__(16) char room[WAVES * WAVE_BYTES];
+    __shared__ float stat[WAVES][2][32];
+    __shared__ uint32_t seen_by[WAVES][32];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
-    const int per = row_tiles * a.kv_heads, number = blockIdx.x / per;
-    const int kv = blockIdx.x % per % a.kv_heads, rt = blockIdx.x % per / a.kv_heads;
-    const int group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
-
-    const int units = chunk_units(a, slots, lane);
-    int s;
-    const int slot0 = first_chunk(a, units, number, s);
-    if (s < 0) return;
-    const int length = length_of(a, s), chunk = units * kUnit;
-    if ((int64_t)(number - slot0) * chunk >= length && number != slot0) return;
-    const int first = (number - slot0) * chunk, end = length - first < chunk ? length : first + chunk;
-    const bool whole = length <= chunk;
-    const int t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s;
-    const int tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
-    const int mine = tokens < a.max_rows ? tokens : a.max_rows;
-    if (rt * 32 >= mine * group) return;
-
-    const int row = rt * 32 + r, token = row / group, head = kv * group + row % group;
-    const bool there = token < mine;
-    const Pages pages = {a.table + s * a.table_row, a.pages, a.table_pages, a.page_bits, kv, a.kv_heads, length};
-    const Tree tree = {a.tree && there ? a.tree + (int64_t)(t0 + token) * a.tree_words : nullptr, a.tree_words, token, length - tokens};
+    const int number = blockIdx.x / a.kv_heads, kv = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
+    Work w;
+    if (!w.find(a, slots, number)) return;
+    const Pages pages = {a.table + w.s * a.table_row, a.pages, a.table_pages, a.page_bits, kv, a.kv_heads, w.length};
     const E *kp = (const E *)a.k_cache, *vp = (const E *)a.v_cache;
+    int j = w.first + wave * 32;
+    int64_t next = j < w.end ? pages.row(j + r) : -1;
+    if (w.mine <= 0) return;
 
-    V8 q[STEPS];
-    {
-        const E *qp = (const E *)a.q.p + (int64_t)(t0 + token) * a.q.row + head * a.q.head;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) q[i] = load_unit8(qp, 2 * i + h, a.dim, there);
-    }
+    const int token = r / group, head = kv * group + r % group;
+    const bool there = token < w.mine;
+    const Tree tree = {a.tree && there ? a.tree + (int64_t)(w.t0 + token) * a.tree_words : nullptr, a.tree_words, token, w.length - w.tokens};
 
     E *ks = reinterpret_cast<E *>(room + wave * WAVE_BYTES), *vs = ks + 32 * HD;
     v4u kr[PIECES], vr[PIECES];
@@ -164,21 +229,20 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel
             vr[i] = ok ? *reinterpret_cast<const v4u *>(vp + at * a.dim + u * T::PER) : v4u{0, 0, 0, 0};
         }
     };
+    if (j < w.end) fetch(next);
+    next = j + STRIDE < w.end ? pages.row(j + STRIDE + r) : -1;
+    V8 q[STEPS];
+    const E *qp = (const E *)a.q.p + (int64_t)(w.t0 + token) * a.q.row + head * a.q.head;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) q[i] = load_unit8(qp, 2 * i + h, a.dim, there);
 
     const float c = a.scale * kLog2e;
     float m = kNoKey, l = 0.0f;
     uint32_t any = 0;
     v16f o[DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-
-    int j = first + wave * 32;
-    int64_t next = j < end ? pages.row(j + r) : -1;
-    if (j < end) fetch(next);
-    next = j + 128 < end ? pages.row(j + 128 + r) : -1;
-    for (; j < end; j += 128) {
+    for (int d = 0; d < DT; ++d) o[d] = zeros();
+    for (; j < w.end; j += STRIDE) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int piece = lane + 64 * i, at = T::place(piece / T::UNITS, piece % T::UNITS);
@@ -186,51 +250,18 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel
             *reinterpret_cast<v4u *>(vs + at) = vr[i];
         }
         wave_order();
-        uint32_t mask = valid & (there ? tree.mask(j) : 0);
-        if (j + 128 < end) {
+        const uint32_t mask = valid & (there ? tree.mask(j) : 0);
+        if (j + STRIDE < w.end) {
             fetch(next);
-            next = j + 256 < end ? pages.row(j + 256 + r) : -1;
+            next = j + 2 * STRIDE < w.end ? pages.row(j + 2 * STRIDE + r) : -1;
         }
         any |= mask;
-        v16f x;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) x = multiply(T::row_operand(ks, r, i, h), q[i], x);
-        if (__any(mask != 0xffffffffu)) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = mask >> (8 * (i / 4) + 4 * h + i % 4) & 1 ? x[i] : -INFINITY;
-        }
-        float most = x[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) most = __builtin_elementwise_maximum(most, x[i]);
-        most = both_max(most) * c;
-        if (__any(most > m + 8.0f)) {
-            const float raised = most > m ? most : m, f = __builtin_amdgcn_exp2f(m - raised);
-            m = raised;
-            l *= f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= f;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m));
-            l += x[i];
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const V8 p = operand_of<E>(x, half);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = multiply(T::column_operand(vs, half * 16, d * 32, lane), p, o[d]);
-        }
+        attend<E, HD, 1>(ks, vs, 0, q, c, m, l, o, [&](v16f (&x)[1]) { hide_keys(x[0], mask, h); });
         wave_order();
     }
 
-    // ---- the four waves' rows: [HD][PITCH] of each in the room of its tiles
+    // ---- the waves' rows: [HD][PITCH] of each in the room of its tiles
     float *mine_o = reinterpret_cast<float *>(room + wave * WAVE_BYTES);
-    __syncthreads();
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -242,21 +273,17 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel
         seen_by[wave][r] = any;
     }
     __syncthreads();
-    const int64_t place = ((int64_t)number * a.kv_heads + kv) * most_rows;
-    float *rows_out = a.partial, *logs = a.partial + (int64_t)(slots + a.sequences) * a.kv_heads * most_rows * a.dim;
-    const int live = mine * group - rt * 32;
-    for (int i = wave; i < 32 && i < live; i += 4) {
+    for (int i = wave; i < 32 && i < w.mine * group; i += WAVES) {
         float top = kNoKey;
         uint32_t seen = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = __builtin_elementwise_maximum(top, stat[w][0][i]), seen |= seen_by[w][i];
-        float f[4], sum = 0.0f;
+        for (int v = 0; v < WAVES; ++v) top = __builtin_elementwise_maximum(top, stat[v][0][i]), seen |= seen_by[v][i];
+        float f[WAVES], sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            f[w] = __builtin_amdgcn_exp2f(stat[w][0][i] - top);
-            sum = __builtin_fmaf(stat[w][1][i], f[w], sum);
+        for (int v = 0; v < WAVES; ++v) {
+            f[v] = __builtin_amdgcn_exp2f(stat[v][0][i] - top);
+            sum = __builtin_fmaf(stat[v][1][i], f[v], sum);
         }
-        const int of = rt * 32 + i;
         float y[2];
         bool bad = false;
 #pragma unroll
@@ -265,91 +292,279 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel
             y[e] = 0.0f;
             if (d < HD) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    y[e] = __builtin_fmaf(reinterpret_cast<const float *>(room + w * WAVE_BYTES)[d * PITCH + i], f[w], y[e]);
+                for (int v = 0; v < WAVES; ++v)
+                    y[e] = __builtin_fmaf(reinterpret_cast<const float *>(room + v * WAVE_BYTES)[d * PITCH + i], f[v], y[e]);
                 y[e] = seen ? y[e] / sum : 0.0f;
             }
             bad |= !is_finite(y[e]);
         }
         float log2 = top + __builtin_amdgcn_logf(sum);
-        if (__any(bad)) {
-            const int tk = of / group;
-            const Tree its = {a.tree ? a.tree + (int64_t)(t0 + tk) * a.tree_words : nullptr, a.tree_words, tk, length - tokens};
-            const CacheKeys<E> keys = {kp, vp, pages, its, first, end - first, a.dim};
-            log2 = row_again<E>((const E *)a.q.p + (int64_t)(t0 + tk) * a.q.row + (kv * group + of % group) * a.q.head, a.dim, c, keys, y);
-        }
-        // (a row whose scores are all -inf is NaN by the formula, but only where no other chunk has more)
-        if (!(log2 > kNoKey) && log2 == log2) log2 = kNoKey;
-        if (whole) {
-            E *to = (E *)a.out.p + (int64_t)(t0 + of / group) * a.out.row + (kv * group + of % group) * a.out.head;
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (lane + 64 * e < a.dim) to[lane + 64 * e] = (E)y[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (lane + 64 * e < a.dim) rows_out[(place + of) * a.dim + lane + 64 * e] = y[e];
-            if (lane == 0) logs[place + of] = seen ? log2 : -INFINITY;
-        }
+        if (__any(bad)) log2 = again<E>(a, w, pages, kv, i, c, y);
+        leave_row<E>(a, w, slots, number, kv, i, seen != 0, log2, y);
     }
 }
 
-// The chunks of a row, weighted by their sums: one workgroup a row of a head, its waves take chunks in turn.
-template <class E>
-__global__ __launch_bounds__(256) void attn_cache_join_kernel(DsqAttnCacheArgs a, int slots)
-{
-    __shared__ float part[4][128], tops[4], sums[4];
-    const int lane = threadIdx.x & 63, wave = wave_number();
-    const int t = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads, group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
-    int s = t;
-    if (a.q_starts) {
-        s = find_sequence(a.q_starts, a.rows, a.sequences, 0, t);
-        if (s < 0) return;
-    }
-    const int t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s, tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
-    if (t < t0 || t - t0 >= tokens || t - t0 >= a.max_rows) return;
-    const int units = chunk_units(a, slots, lane), length = length_of(a, s), chunk = units * kUnit;
-    if (length <= chunk) return;
-    int of = s;
-    const int slot0 = first_chunk(a, units, -1, of), chunks = (length + chunk - 1) / chunk;
-    const int64_t step = (int64_t)a.kv_heads * most_rows;
-    const int64_t place = slot0 * step + (int64_t)(head / group) * most_rows + (t - t0) * group + head % group;
-    const float *logs = a.partial + (int64_t)(slots + a.sequences) * step * a.dim + place, *rows = a.partial + place * a.dim;
+// ---- more rows: four waves take 32 each, over tiles of keys that they share ------------------------------------
 
-    float top = -INFINITY;
-    for (int i = lane; i < chunks; i += 64) top = __builtin_elementwise_maximum(top, logs[i * step]);
-    for (int off = 32; off > 0; off >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, off));
-    float y0 = 0.0f, y1 = 0.0f, sum = 0.0f;
-    if (top != -INFINITY) {
-#pragma unroll 4
-        for (int i = wave; i < chunks; i += 4) {
-            const float f = __builtin_amdgcn_exp2f(logs[i * step] - top);
-            const float v0 = lane < a.dim ? rows[i * step * a.dim + lane] : 0.0f, v1 = lane + 64 < a.dim ? rows[i * step * a.dim + lane + 64] : 0.0f;
-            sum += f;
-            // (a chunk of no weight may hold NaN)
-            y0 = f == 0.0f ? y0 : __builtin_fmaf(f, v0, y0);
-            y1 = f == 0.0f ? y1 : __builtin_fmaf(f, v1, y1);
+template <class E, int HD>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_kernel(DsqAttnCacheArgs a, int slots, int row_tiles)
+{
+    typedef Tile<E, HD> T;
+    typedef typename Operand<E>::type V8;
+    constexpr int STEPS = HD / 16, DT = HD / 32, KT = sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT, TILE = KEYS * HD;
+    constexpr int PIECES = KEYS * T::UNITS / 256, STEP = 256 / T::UNITS;
+    __shared__ __align__(16) E tiles_at[2][2][TILE];
+    __shared__ uint32_t there_at[2][KT];
+    static_assert(32 * HD * 4 <= (int)sizeof(E) * TILE, "a wave's rows fit a tile");
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
+    const int kv = blockIdx.x % a.kv_heads, number = blockIdx.x / a.kv_heads / row_tiles, rt = blockIdx.x / a.kv_heads % row_tiles;
+    const int group = a.q_heads / a.kv_heads;
+    Work w;
+    if (!w.find(a, slots, number) || rt * 128 >= w.mine * group) return;
+    const Pages pages = {a.table + w.s * a.table_row, a.pages, a.table_pages, a.page_bits, kv, a.kv_heads, w.length};
+    const E *kp = (const E *)a.k_cache, *vp = (const E *)a.v_cache;
+
+    const int row0 = rt * 128 + wave * 32, row = row0 + r, token = row / group, head = kv * group + row % group;
+    const bool there = token < w.mine, busy = row0 < w.mine * group;
+    const Tree tree = {a.tree && there ? a.tree + (int64_t)(w.t0 + token) * a.tree_words : nullptr, a.tree_words, token, w.length - w.tokens};
+    V8 q[STEPS];
+    const E *qp = (const E *)a.q.p + (int64_t)(w.t0 + token) * a.q.row + head * a.q.head;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) q[i] = load_unit8(qp, 2 * i + h, a.dim, there);
+
+    // A thread moves 16 bytes of the rows tid / UNITS + STEP i of a tile; a place is looked up one tile before its load.  Where pages
+    // hold whole tiles, there is one place for all.
+    const int u = tid % T::UNITS, from = tid / T::UNITS;
+    const bool one = (1 << a.page_bits) >= KEYS;
+    v4u kr[PIECES], vr[PIECES];
+    int64_t place[PIECES];
+    auto look = [&](int j) {
+        if (one) {
+            place[0] = j < w.end ? pages.row(j) : -1;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) place[i] = j + from + STEP * i < w.end ? pages.row(j + from + STEP * i) : -1;
+    };
+    uint32_t valid = 0;                      // bit i: of piece i
+    const auto load = [&](const E *p, int64_t at, bool ok) {
+        return ok && u * T::PER < a.dim ? *reinterpret_cast<const v4u *>(p + at * a.dim + u * T::PER) : v4u{0, 0, 0, 0};
+    };
+    auto fetch = [&](int j) {
+        valid = 0;
+        if (one) {
+            const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane((int)(place[0] >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)place[0]);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int row = from + STEP * i;
+                const bool ok = first >= 0 && j + row < w.end;
+                valid |= (ok ? 1u : 0u) << i;
+                kr[i] = load(kp + first * a.dim, row, ok);
+                vr[i] = load(vp + first * a.dim, row, ok);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            valid |= (place[i] >= 0 ? 1u : 0u) << i;
+            kr[i] = load(kp, place[i], place[i] >= 0);
+            vr[i] = load(vp, place[i], place[i] >= 0);
+        }
+    };
+
+    const float c = a.scale * kLog2e;
+    float m = kNoKey, l = 0.0f;
+    uint32_t any = 0;
+    v16f o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = zeros();
+    look(w.first);
+    fetch(w.first);
+    look(w.first + KEYS);
+    if (tid < 2 * KT) there_at[tid / KT][tid % KT] = 0;
+    __syncthreads();
+    int b = 0;
+    for (int j = w.first; j < w.end; j += KEYS, b ^= 1) {
+        E *const kt = tiles_at[b][0], *const vt = tiles_at[b][1];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = T::place(from + STEP * i, u), key = from + STEP * i;
+            *reinterpret_cast<v4u *>(kt + at) = kr[i];
+            *reinterpret_cast<v4u *>(vt + at) = vr[i];
+            if (u == 0 && (valid >> i & 1)) atomicOr(&there_at[b][key / 32], 1u << key % 32);
+        }
+        __syncthreads();
+        uint32_t mask[KT];
+#pragma unroll
+        for (int n = 0; n < KT; ++n) mask[n] = there_at[b][n] & (there ? tree.mask(j + n * 32) : 0);
+        if (j + KEYS < w.end) {
+            fetch(j + KEYS);
+            look(j + 2 * KEYS);
+        }
+#pragma unroll
+        for (int n = 0; n < KT; ++n) any |= mask[n];
+        if (busy)
+            attend<E, HD, KT>(kt, vt, 0, q, c, m, l, o, [&](v16f (&x)[KT]) {
+#pragma unroll
+                for (int n = 0; n < KT; ++n) hide_keys(x[n], mask[n], h);
+            });
+        // (the other buffer's bits are read before the barrier that comes, and set after it)
+        if (tid < KT) there_at[b ^ 1][tid] = 0;
+        __syncthreads();
+    }
+    if (!busy) return;
+
+    // The rows lie transposed in registers: through LDS, a wave's in the room of its tile (units exchanged as in a tile).
+    float *mine_o = reinterpret_cast<float *>(&tiles_at[0][0][0]) + wave * TILE * (int)sizeof(E) / 4;
+    l = both_sum(l);
+    const float inv = any ? 1.0f / l : 0.0f, log2 = m + __builtin_amdgcn_logf(l);
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (any) y = v4f{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * inv;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= !is_finite(y[e]);
+            *reinterpret_cast<v4f *>(mine_o + r * HD + ((d * 8 + 2 * i + h) ^ (r % (HD / 4))) * 4) = y;
+        }
+    wave_order();
+    const int most_rows = a.max_rows * group;
+    const int64_t rows_at = ((int64_t)number * a.kv_heads + kv) * most_rows + row0;
+    constexpr int ACROSS = HD / 4, DOWN = 64 / ACROSS;          // lanes of a row, rows of a step
+#pragma unroll
+    for (int i = 0; i < 32; i += DOWN) {
+        const int its = i + lane / ACROSS, at = lane % ACROSS;
+        const v4f y = *reinterpret_cast<const v4f *>(mine_o + its * HD + (at ^ (its % (HD / 4))) * 4);
+        const int of = row0 + its;
+        if (of >= w.mine * group || at * 4 >= a.dim) continue;
+        if (w.whole) {
+            Side<E, 4> v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v.at[e] = (E)y[e];
+            store_side((E *)a.out.p + (int64_t)(w.t0 + of / group) * a.out.row + (kv * group + of % group) * a.out.head + at * 4, v);
+        } else {
+            *reinterpret_cast<v4f *>(a.partial + (rows_at + its) * a.dim + at * 4) = y;
         }
     }
-    part[wave][lane] = y0;
-    part[wave][lane + 64] = y1;
-    if (lane == 0) sums[wave] = sum;
-    __syncthreads();
-    const int d = threadIdx.x;
-    if (d < a.dim) {
-        const float total = sums[0] + sums[1] + sums[2] + sums[3], y = part[0][d] + part[1][d] + part[2][d] + part[3][d];
-        ((E *)a.out.p)[(int64_t)t * a.out.row + head * a.out.head + d] = (E)(top == -INFINITY ? 0.0f : y / total);
+    if (!w.whole && there && h == 0) logs_of(a, slots, kv, row)[number] = any ? log2 > kNoKey || log2 != log2 ? log2 : kNoKey : -INFINITY;
+    uint64_t spoilt = __ballot(bad && there);
+    spoilt = (spoilt | spoilt >> 32) & 0xffffffffu;
+    while (spoilt) {
+        const int i = __ffsll((unsigned long long)spoilt) - 1;
+        spoilt &= spoilt - 1;
+        float y[2];
+        const float its = again<E>(a, w, pages, kv, row0 + i, c, y);
+        leave_row<E>(a, w, slots, number, kv, row0 + i, true, its, y);
+    }
+}
+
+// The chunks of a row, weighted by their sums.  WAVES waves take the chunks of a row in turn, or (WAVES = 1) a wave takes HEADS heads at once.
+template <class E, int WAVES, int HEADS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join_kernel(DsqAttnCacheArgs a, int slots)
+{
+    static_assert(WAVES == 1 || HEADS == 1, "");
+    constexpr int AT_ONCE = HEADS == 1 ? 8 : 4;
+    __shared__ float part[WAVES == 1 ? 1 : WAVES][128];
+    const int lane = threadIdx.x & 63, wave = wave_number(), group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
+    const int turns = (a.q_heads + HEADS - 1) / HEADS;
+    const int64_t unit = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+    const int t = (int)(unit / turns), head0 = (int)(unit % turns) * HEADS, turn = WAVES == 1 ? 0 : wave;
+    if (t >= a.rows) return;
+    int s = t, units;
+    if (a.q_starts) s = find_sequence(a.q_starts, a.rows, a.sequences, 0, t);
+    if (s < 0) return;
+    int of = s;
+    const int slot0 = first_chunk(a, slots, -1, of, units);
+    const int t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s, tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
+    const int length = length_of(a, s), chunk = units * kUnit, chunks = (length + chunk - 1) / chunk;
+    if (t < t0 || t - t0 >= tokens || t - t0 >= a.max_rows || chunks <= 1) return;
+    const int64_t step = (int64_t)a.kv_heads * most_rows * a.dim;
+    const int d0 = lane < a.dim ? lane : 0, d1 = lane + 64 < a.dim ? lane + 64 : 0;
+    const float *logs[HEADS], *rows[HEADS];
+    float top[HEADS], y0[HEADS], y1[HEADS], sum[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        const int head = head0 + i < a.q_heads ? head0 + i : a.q_heads - 1, row = (t - t0) * group + head % group;
+        logs[i] = logs_of(a, slots, head / group, row) + slot0;
+        rows[i] = a.partial + slot0 * step + ((int64_t)(head / group) * most_rows + row) * a.dim;
+        top[i] = -INFINITY;
+        y0[i] = y1[i] = sum[i] = 0.0f;
+    }
+    for (int c = 0; c < chunks; c += 64)
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) top[i] = __builtin_elementwise_maximum(top[i], c + lane < chunks ? logs[i][c + lane] : -INFINITY);
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        for (int off = 32; off > 0; off >>= 1) top[i] = __builtin_elementwise_maximum(top[i], __shfl_xor(top[i], off));
+        top[i] = top[i] == -INFINITY ? 0.0f : top[i];            // (no chunk has a key that the row sees: all weights are zero)
+    }
+    for (int base = 0; base < chunks; base += 64) {
+        float f[HEADS];
+        const int n = chunks - base < 64 ? chunks - base : 64;
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            f[i] = lane < n ? __builtin_amdgcn_exp2f(logs[i][base + lane] - top[i]) : 0.0f;
+            sum[i] += f[i];
+        }
+        for (int c0 = turn; c0 < n; c0 += AT_ONCE * WAVES) {
+            // (loads of several chunks under way; those past the last have no weight)
+            float v0[AT_ONCE][HEADS], v1[AT_ONCE][HEADS];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int c = c0 + k * WAVES < n ? c0 + k * WAVES : c0;
+#pragma unroll
+                for (int i = 0; i < HEADS; ++i) v0[k][i] = rows[i][(base + c) * step + d0], v1[k][i] = rows[i][(base + c) * step + d1];
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                for (int i = 0; i < HEADS; ++i) {
+                    const float p = c0 + k * WAVES < n ? __shfl(f[i], (c0 + k * WAVES) & 63) : 0.0f;
+                    // (a chunk of no weight may hold NaN)
+                    y0[i] = p == 0.0f ? y0[i] : __builtin_fmaf(p, v0[k][i], y0[i]);
+                    y1[i] = p == 0.0f ? y1[i] : __builtin_fmaf(p, v1[k][i], y1[i]);
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+        for (int off = 32; off > 0; off >>= 1) sum[i] += __shfl_xor(sum[i], off);
+    if (WAVES > 1) {
+        part[wave][lane] = y0[0];
+        part[wave][lane + 64] = y1[0];
+        __syncthreads();
+        if (turn > 0) return;
+        y0[0] = y1[0] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) y0[0] += part[w][lane], y1[0] += part[w][lane + 64];
+    }
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        if (head0 + i >= a.q_heads) return;
+        E *to = (E *)a.out.p + (int64_t)t * a.out.row + (head0 + i) * a.out.head;
+        if (lane < a.dim) to[lane] = (E)(sum[i] == 0.0f ? 0.0f : y0[i] / sum[i]);
+        if (lane + 64 < a.dim) to[lane + 64] = (E)(sum[i] == 0.0f ? 0.0f : y1[i] / sum[i]);
     }
 }
 
 template <class E, int HD>
 hipError_t launch(const DsqAttnCacheArgs &a, hipStream_t stream)
 {
-    const AttnCachePlan p = attn_cache_plan(a.max_rows, a.q_heads, a.kv_heads);
-    const int64_t groups = (int64_t)(p.slots + a.sequences) * p.row_tiles * a.kv_heads;
-    attn_cache_kernel<E, HD><<<(unsigned)groups, 256, 0, stream>>>(a, p.slots, p.row_tiles);
+    const AttnCachePlan p = attn_cache_plan(a.max_rows, a.q_heads, a.kv_heads, a.sequences, (int64_t)a.table_pages << a.page_bits);
+    const unsigned groups = (unsigned)((int64_t)(p.slots + a.sequences) * p.row_tiles * a.kv_heads);
+    if (p.tiles) attn_cache_tiles_kernel<E, HD><<<groups, 256, 0, stream>>>(a, p.slots, p.row_tiles);
+    else if (p.single) attn_cache_kernel<E, HD, sizeof(E) == 2 ? 8 : 4><<<groups, sizeof(E) == 2 ? 512 : 256, 0, stream>>>(a, p.slots);
+    else attn_cache_kernel<E, HD, 4><<<groups, 256, 0, stream>>>(a, p.slots);
     if (const hipError_t e = hipGetLastError()) return e;
-    attn_cache_join_kernel<E><<<(unsigned)((int64_t)a.rows * a.q_heads), 256, 0, stream>>>(a, p.slots);
+    if (p.single) return hipSuccess;
+    // Many chunks a row: a workgroup of 16 waves each; a few: a wave takes one row, or four where there are many.
+    const int64_t rows = (int64_t)a.rows * a.q_heads, fours = (int64_t)a.rows * ((a.q_heads + 3) / 4);
+    if (p.slots / a.sequences >= 16 && rows <= 1024) attn_cache_join_kernel<E, 16, 1><<<(unsigned)rows, 1024, 0, stream>>>(a, p.slots);
+    else if (rows <= 4096) attn_cache_join_kernel<E, 1, 1><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a, p.slots);
+    else attn_cache_join_kernel<E, 1, 4><<<(unsigned)((fours + 3) / 4), 256, 0, stream>>>(a, p.slots);
     return hipGetLastError();
 }
 
@@ -363,7 +578,8 @@ hipError_t of_dim(const DsqAttnCacheArgs &a, hipStream_t stream)
 
 size_t dsq_attn_cache_floats(int sequences, int max_rows, int q_heads, int kv_heads, int dim)
 {
-    const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads);
+    // (the room does not go by the table's size: as many chunks as any call has)
+    const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads, sequences, INT64_MAX);
     return (size_t)(p.slots + sequences) * max_rows * q_heads * (dim + 1);
 }
 

@@ -1,16 +1,24 @@
 // Plan of a call of attention over a paged cache (host arithmetic).
 #pragma once
+#include <stdint.h>
 
 struct AttnCachePlan {
-    int slots, row_tiles;                    // chunks that all keys are cut into, at most that many and one more a sequence; tiles of 32 rows
+    bool tiles;                              // more than 32 rows a key head: four waves share tiles of keys
+    bool single;                             // every sequence is one chunk: nothing to join
+    int row_tiles, slots;                    // tiles of rows; chunks that all keys are cut into (and one more a sequence); 0: single
 };
 
-// Two workgroups share a compute unit: 512 fill the card.
-inline AttnCachePlan attn_cache_plan(int max_rows, int q_heads, int kv_heads)
+// `keys`: the most that a sequence can have.
+inline AttnCachePlan attn_cache_plan(int max_rows, int q_heads, int kv_heads, int sequences, int64_t keys)
 {
     AttnCachePlan p;
-    p.row_tiles = (int)(((long long)max_rows * (q_heads / kv_heads) + 31) / 32);
-    const long long others = (long long)p.row_tiles * kv_heads;
-    p.slots = others >= 512 ? 1 : (int)(512 / others);
+    const int64_t rows = (int64_t)max_rows * (q_heads / kv_heads);
+    p.tiles = rows > 32;
+    p.row_tiles = p.tiles ? (int)((rows + 127) / 128) : 1;
+    const int64_t others = (int64_t)p.row_tiles * kv_heads;
+    const int64_t most = p.tiles ? 512 : 1024;
+    p.slots = others >= most ? 1 : (int)(most / others);
+    p.single = !p.tiles && keys <= 1024;
+    if (p.single) p.slots = 0;
     return p;
 }

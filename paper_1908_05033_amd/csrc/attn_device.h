@@ -106,14 +106,23 @@ struct Mover {
     v4u at[PIECES];
     // Rows first .. first + ROWS - 1 of `p`; the last before `end` again from there on (what they are worth, the caller leaves out), and
     // the first unit again past the elements of a head (their products meet zeros or are not stored): no load is behind a branch.
+    // Whole tiles take one offset for all lanes' pieces and addresses that the scalar unit forms.
     __device__ __forceinline__ void fetch(const E *p, int64_t stride, int first, int end, int dim)
     {
-        const int u = threadIdx.x % T::UNITS, j = first + (int)(threadIdx.x / T::UNITS);
-        const E *from = p + (u * T::PER < dim ? u * T::PER : 0);
+        int u = threadIdx.x % T::UNITS;
+        const int row = threadIdx.x / T::UNITS;
+        u = u * T::PER < dim ? u * T::PER : 0;
+        if (first + ROWS <= end && stride <= 1 << 24) {
+            const uint32_t off = ((uint32_t)row * (uint32_t)stride + u) * (uint32_t)sizeof(E);
+            const char *from = reinterpret_cast<const char *>(p + first * stride);
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int row = j + STEP * i < end ? j + STEP * i : end - 1;
-            at[i] = *reinterpret_cast<const v4u *>(from + row * stride);
+            for (int i = 0; i < PIECES; ++i) at[i] = *reinterpret_cast<const v4u *>(from + i * STEP * stride * (int)sizeof(E) + off);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int j = first + row + STEP * i;
+                at[i] = *reinterpret_cast<const v4u *>(p + u + (j < end ? j : end - 1) * stride);
+            }
         }
     }
     __device__ __forceinline__ void put(E *t) const
@@ -272,6 +281,57 @@ __device__ __forceinline__ int visible(const Sequence &s, int causal, int i)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A softmax's reference before its first key: below every score, and finite, so that differences with it are numbers.
 constexpr float kNoKey = -3.0e38f;
+
+// ---- a block of keys ----------------------------------------------------------------------------------
+//
+// 32 KT keys, from row `in` of the tiles kt and vt on, for the 32 rows of a wave: running maximum m and sum l (of the scores times c, to
+// base 2) of the lane's row and the transposed sums o.  `hide` puts -inf in the place of scores that are not seen.
+template <class E, int HD, int KT, class Hide>
+__device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[HD / 16], float c, float &m, float &l,
+                                       v16f (&o)[HD / 32], Hide hide)
+{
+    typedef Tile<E, HD> T;
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    v16f x[KT];
+#pragma unroll
+    for (int n = 0; n < KT; ++n) {
+        x[n] = zeros();
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
+    }
+    hide(x);
+    float most = x[0][0];
+#pragma unroll
+    for (int n = 0; n < KT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = __builtin_elementwise_maximum(most, x[n][i]);
+    most = both_max(most) * c;
+    // The reference is raised only where a score passes it by 2^8: up to there sums and operands lose nothing.
+    if (__any(most > m + 8.0f)) {
+        const float next = most > m ? most : m, f = __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+    }
+#pragma unroll
+    for (int n = 0; n < KT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, -m));
+            l += x[n][i];
+        }
+#pragma unroll
+    for (int n = 0; n < KT; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const typename Operand<E>::type p = operand_of<E>(x[n], half);
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
+        }
+}
 
 // ---- a row formed again ---------------------------------------------------------------------------
 //

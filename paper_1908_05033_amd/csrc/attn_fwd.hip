@@ -6,6 +6,8 @@
 // wave 32 of them; tiles of keys and values go through LDS, the next tile's loads under way.  Scores are formed transposed, K Q^T,
 // so that a lane holds one row's scores: maximum, sum and the factor of a raised maximum need no exchange but one between the two
 // lanes of a row, and the probabilities are the second operand of V^T P^T as they lie in registers (attn_device.h).
+#include <type_traits>
+
 #include "attn_device.h"
 
 namespace {
@@ -77,64 +79,30 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64)
     v16f o[F::DT];
 #pragma unroll
     for (int d = 0; d < F::DT; ++d) o[d] = zeros();
-    if (count > 0) fetch(0);
-    for (int t = 0; t < count; ++t) {
-        E *const kt = reinterpret_cast<E *>(room) + (F::BUFFERS == 2 ? t & 1 : 0) * 2 * F::TILE, *const vt = kt + F::TILE;
+    // one block of keys, in a buffer whose place the compiler knows
+    const auto block = [&](int t, auto buffer) {
+        E *const kt = reinterpret_cast<E *>(room) + decltype(buffer)::value * 2 * F::TILE, *const vt = kt + F::TILE;
         if (F::BUFFERS == 1) __syncthreads();
         km.put(kt);
         vm.put(vt);
         __syncthreads();
         if (t + 1 < count) fetch(t + 1);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
-        if (at < any) {
-            v16f x[F::KT];
-#pragma unroll
-            for (int n = 0; n < F::KT; ++n) {
-                x[n] = zeros();
-#pragma unroll
-                for (int i = 0; i < F::STEPS; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
-            }
-            if (at + 32 * F::KT > whole) {
+        if (at < any)
+            attend<E, HD, F::KT>(kt, vt, in, q, c, m, l, o, [&](v16f (&x)[F::KT]) {
+                if (at + 32 * F::KT <= whole) return;
                 stay_a_branch();
                 const int left = seen - at - 4 * h;
 #pragma unroll
                 for (int n = 0; n < F::KT; ++n)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[n][i] = n * 32 + 8 * (i / 4) + i % 4 < left ? x[n][i] : -INFINITY;
-            }
-            float most = x[0][0];
-#pragma unroll
-            for (int n = 0; n < F::KT; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = __builtin_elementwise_maximum(most, x[n][i]);
-            most = both_max(most) * c;
-            // The reference is raised only where a score passes it by 2^8: up to there sums and operands lose nothing.
-            if (__any(most > m + 8.0f)) {
-                const float next = most > m ? most : m, f = __builtin_amdgcn_exp2f(m - next);
-                m = next;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < F::DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
-            }
-#pragma unroll
-            for (int n = 0; n < F::KT; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, -m));
-                    l += x[n][i];
-                }
-#pragma unroll
-            for (int n = 0; n < F::KT; ++n)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const V8 p = operand_of<E>(x[n], half);
-#pragma unroll
-                    for (int d = 0; d < F::DT; ++d)
-                        o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
-                }
-        }
+            });
+    };
+    if (count > 0) fetch(0);
+    for (int t = 0; t < count; t += 2) {
+        block(t, std::integral_constant<int, 0>());
+        if (t + 1 < count) block(t + 1, std::integral_constant<int, F::BUFFERS - 1>());
     }
 
     l = both_sum(l);
