@@ -12,20 +12,28 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                // the most of a workgroup
+constexpr int kRows = 8;                     // the most rows of a workgroup
 
-// What a lane holds: which head of a row, and which units of it.
+// What a workgroup takes: all heads of `rows` rows, or `heads` of one.
+struct Share {
+    int rows, heads, blocks, threads;
+};
+
+// What a lane holds: which head of which of the workgroup's rows, and which units of it.
 struct Place {
-    int unit, c, a, b;                       // unit: q heads, k heads, v heads; c: lane of the head; a, b: units of eight elements, or -1
+    int row, unit, c, a, b;                  // unit: q heads, k heads, v heads; c: lane of the head; a, b: units of eight elements, or -1
     bool turns;
 };
 
 template <int LANES>
-__device__ __forceinline__ Place place_of(int thread, int dim, int pairs, int interleaved)
+__device__ __forceinline__ Place place_of(const Share &share, int dim, int pairs, int interleaved)
 {
     Place p;
-    p.unit = thread / LANES;
-    p.c = thread % LANES;
+    const int item = threadIdx.x / LANES;
+    p.row = item / share.heads;
+    p.unit = p.row < share.rows ? blockIdx.y * share.heads + item % share.heads : 1 << 30;
+    p.c = threadIdx.x % LANES;
     const int turning = pairs / 8;
     p.turns = p.c < turning;
     const bool halves = p.turns && !interleaved;
@@ -80,18 +88,20 @@ __device__ __forceinline__ float rms_of(const float *x, int dim, float eps)
     return (float)(y * __builtin_fma(-0.5 * mean * y, y, 1.5));
 }
 
-// Cosine and sine of the pairs of a row.
+// Cosine and sine of the pairs of `count` rows from `row` on, 256 numbers a row.
 __device__ __forceinline__ void angles(float *table, const int32_t *positions, const uint8_t *pair_axis, const float *frequencies, int rows, int axes,
-                                       int pairs, int row)
+                                       int pairs, int row, int count)
 {
-    for (int j = threadIdx.x; j < pairs; j += kThreads) {
+    for (int i = threadIdx.x; i < pairs * count; i += blockDim.x) {
+        const int r = count == 1 ? 0 : i / pairs, j = i - r * pairs;
+        if (row + r >= rows) return;
         int axis = pair_axis ? pair_axis[j] : 0;
         axis = axis < axes ? axis : axes - 1;
-        const double turns = (double)positions[(int64_t)axis * rows + row] * (double)frequencies[j] * 0.31830988618379067154;
+        const double turns = (double)positions[(int64_t)axis * rows + row + r] * (double)frequencies[j] * 0.31830988618379067154;
         float s, c;
         sincospif((float)(turns - 2.0 * rint(0.5 * turns)), &s, &c);
-        table[2 * j] = c;
-        table[2 * j + 1] = s;
+        table[r * 256 + 2 * j] = c;
+        table[r * 256 + 2 * j + 1] = s;
     }
 }
 
@@ -131,28 +141,26 @@ __device__ __forceinline__ void turn(float *x, const float *table, const Place &
 }
 
 template <class E, int LANES>
-__global__ __launch_bounds__(kThreads) void head_rope_kernel(DsqRopeArgs a)
+__global__ __launch_bounds__(kThreads) void head_rope_kernel(DsqRopeArgs a, Share share)
 {
     typedef typename Operand<E>::type V8;
-    __shared__ __align__(16) float table[256];
-    const int row = blockIdx.x, units = a.q_heads + a.kv_heads + (a.cache.k ? a.kv_heads : 0);
-    const Place p = place_of<LANES>(blockIdx.y * kThreads + threadIdx.x, a.dim, a.pairs, a.interleaved);
-    const bool there = p.unit < units, is_q = p.unit < a.q_heads, is_v = p.unit >= a.q_heads + a.kv_heads;
+    __shared__ __align__(16) float table[kRows * 256];
+    const int row0 = blockIdx.x * share.rows, units = a.q_heads + a.kv_heads + (a.cache.k ? a.kv_heads : 0);
+    const Place p = place_of<LANES>(share, a.dim, a.pairs, a.interleaved);
+    const int row = row0 + p.row;
+    const bool there = p.unit < units && row < a.rows, is_q = p.unit < a.q_heads, is_v = p.unit >= a.q_heads + a.kv_heads;
     const int head = is_q ? p.unit : is_v ? p.unit - a.q_heads - a.kv_heads : p.unit - a.q_heads;
     const DsqHeads in = is_q ? a.q : is_v ? a.v : a.k;
-    const E *from = (const E *)in.p + row * in.row + head * in.head;
     V8 lo = {}, hi = {};
-    if (there) load16(from, p, a.dim, lo, hi);
-    E *cached = nullptr;
-    if (a.cache.k && there && !is_q) {
-        const int64_t slot = a.cache.slots[row], page = slot >> a.cache.page_bits;
-        if (slot >= 0 && page < a.cache.pages)
-            cached = (E *)(is_v ? a.cache.v : a.cache.k) +
-                     (((page * a.kv_heads + head) << a.cache.page_bits) + (slot & ((1 << a.cache.page_bits) - 1))) * a.dim;
+    int64_t slot = -1;
+    if (there) {
+        load16((const E *)in.p + row * in.row + head * in.head, p, a.dim, lo, hi);
+        if (a.cache.k && !is_q) slot = a.cache.slots[row];
     }
-    angles(table, a.positions, a.pair_axis, a.frequencies, a.rows, a.axes, a.pairs, row);
+    angles(table, a.positions, a.pair_axis, a.frequencies, a.rows, a.axes, a.pairs, row0, share.rows);
     __syncthreads();
-    if (there && !is_v) {
+    if (!there) return;
+    if (!is_v) {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)lo[i], x[i + 8] = (float)hi[i];
@@ -167,66 +175,78 @@ __global__ __launch_bounds__(kThreads) void head_rope_kernel(DsqRopeArgs a)
                 x[i + 8] = x[i + 8] * r * (weight ? (float)wh[i] : 1.0f);
             }
         }
-        turn(x, table, p, a.interleaved, 1.0f);
+        turn(x, table + p.row * 256, p, a.interleaved, 1.0f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) lo[i] = (E)x[i], hi[i] = (E)x[i + 8];
+        const DsqHeadsOut out = is_q ? a.q_out : a.k_out;
+        if (out.p) {
+            E *to = (E *)out.p + row * out.row + head * out.head;
+            if (p.a >= 0) store8(to + 8 * p.a, lo);
+            if (p.b >= 0) store8(to + 8 * p.b, hi);
+        }
     }
-    if (!there) return;
-    const DsqHeadsOut out = is_q ? a.q_out : a.k_out;
-    E *to = is_v || !out.p ? nullptr : (E *)out.p + row * out.row + head * out.head;
-    if (to && p.a >= 0) store8(to + 8 * p.a, lo);
-    if (to && p.b >= 0) store8(to + 8 * p.b, hi);
-    if (cached && p.a >= 0) store8(cached + 8 * p.a, lo);
-    if (cached && p.b >= 0) store8(cached + 8 * p.b, hi);
+    const int64_t page = slot >> a.cache.page_bits;
+    if (slot >= 0 && page < a.cache.pages) {
+        E *to = (E *)(is_v ? a.cache.v : a.cache.k) + (((page * a.kv_heads + head) << a.cache.page_bits) + (slot & ((1 << a.cache.page_bits) - 1))) * a.dim;
+        if (p.a >= 0) store8(to + 8 * p.a, lo);
+        if (p.b >= 0) store8(to + 8 * p.b, hi);
+    }
 }
 
-// A workgroup takes rows in turn and keeps the weights' gradients of its heads in registers.
+// A workgroup takes its rows in turn, the next ones' heads and angles under way, and keeps the weights' gradients of its heads in registers.
 template <class E, int LANES>
-__global__ __launch_bounds__(kThreads) void head_rope_bwd_kernel(DsqRopeBwdArgs a)
+__global__ __launch_bounds__(kThreads) void head_rope_bwd_kernel(DsqRopeBwdArgs a, Share share)
 {
     typedef typename Operand<E>::type V8;
-    constexpr int HEADS = kThreads / LANES, WIDE = LANES * 16;
-    __shared__ __align__(16) float table[2][256];
-    __shared__ float sums[HEADS * WIDE];
+    constexpr int WIDE = LANES * 16;
+    __shared__ __align__(16) float table[2][kRows * 256];
+    __shared__ float sums[kThreads * 16];
     const int units = a.q_heads + a.kv_heads;
-    const Place p = place_of<LANES>(blockIdx.y * kThreads + threadIdx.x, a.dim, a.pairs, a.interleaved);
-    const bool there = p.unit < units, is_q = p.unit < a.q_heads;
+    const Place p = place_of<LANES>(share, a.dim, a.pairs, a.interleaved);
+    const bool mine = p.unit < units, is_q = p.unit < a.q_heads;
     const int head = is_q ? p.unit : p.unit - a.q_heads;
     const DsqHeads in = is_q ? a.q : a.k, grad = is_q ? a.grad_q_out : a.grad_k_out;
     const DsqHeadsOut out = is_q ? a.grad_q : a.grad_k;
     const E *weight = (const E *)(is_q ? a.q_weight : a.k_weight);
-    float w[16], gw[16];
-    {
-        V8 wl, wh;
-        if (weight) load16(weight, p, a.dim, wl, wh);
+    V8 wl, wh;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = weight ? (float)wl[i] : 1.0f, w[i + 8] = weight ? (float)wh[i] : 1.0f;
-    }
+    for (int i = 0; i < 8; ++i) wl[i] = wh[i] = (E)1.0f;
+    if (weight) load16(weight, p, a.dim, wl, wh);
+    float gw[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) gw[i] = 0.0f;
-    int turns = 0;
-    for (int row = blockIdx.x; row < a.rows; row += gridDim.x, turns ^= 1) {
-        V8 xl = {}, xh = {}, gl = {}, gh = {};
-        if (there) {
+
+    V8 xl = {}, xh = {}, gl = {}, gh = {};
+    auto fetch = [&](int row) {
+        if (mine && row < a.rows) {
             load16((const E *)grad.p + row * grad.row + head * grad.head, p, a.dim, gl, gh);
             if (a.eps > 0.0f) load16((const E *)in.p + row * in.row + head * in.head, p, a.dim, xl, xh);
         }
-        angles(table[turns], a.positions, a.pair_axis, a.frequencies, a.rows, a.axes, a.pairs, row);
+    };
+    const int step = gridDim.x * share.rows;
+    int b = 0, row0 = blockIdx.x * share.rows;
+    fetch(row0 + p.row);
+    angles(table[0], a.positions, a.pair_axis, a.frequencies, a.rows, a.axes, a.pairs, row0, share.rows);
+    for (; row0 < a.rows; row0 += step, b ^= 1) {
+        const int row = row0 + p.row;
+        const bool there = mine && row < a.rows;
+        float g[16], x[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = (float)gl[i], g[i + 8] = (float)gh[i], x[i] = (float)xl[i], x[i + 8] = (float)xh[i];
         __syncthreads();
-        float g[16];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = (float)gl[i], g[i + 8] = (float)gh[i];
-        turn(g, table[turns], p, a.interleaved, -1.0f);
+        if (row0 + step < a.rows) {
+            fetch(row + step);
+            angles(table[b ^ 1], a.positions, a.pair_axis, a.frequencies, a.rows, a.axes, a.pairs, row0 + step, share.rows);
+        }
+        turn(g, table[b] + p.row * 256, p, a.interleaved, -1.0f);
         if (a.eps > 0.0f) {
-            float x[16], dot = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (float)xl[i], x[i + 8] = (float)xh[i];
+            float dot = 0.0f;
             const float r = rms_of<LANES>(x, a.dim, a.eps);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 x[i] *= r;
-                gw[i] = __builtin_fmaf(g[i], x[i], gw[i]);
-                g[i] *= w[i];
+                if (there) gw[i] = __builtin_fmaf(g[i], x[i], gw[i]);
+                g[i] *= (float)(i < 8 ? wl[i % 8] : wh[i % 8]);
                 dot = __builtin_fmaf(g[i], x[i], dot);
             }
             dot = lanes_sum<LANES>(dot) / a.dim;
@@ -234,16 +254,17 @@ __global__ __launch_bounds__(kThreads) void head_rope_bwd_kernel(DsqRopeBwdArgs 
             for (int i = 0; i < 16; ++i) g[i] = r * __builtin_fmaf(-x[i], dot, g[i]);
         }
         if (there) {
+            V8 lo, hi;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) gl[i] = (E)g[i], gh[i] = (E)g[i + 8];
+            for (int i = 0; i < 8; ++i) lo[i] = (E)g[i], hi[i] = (E)g[i + 8];
             E *to = (E *)out.p + row * out.row + head * out.head;
-            if (p.a >= 0) store8(to + 8 * p.a, gl);
-            if (p.b >= 0) store8(to + 8 * p.b, gh);
+            if (p.a >= 0) store8(to + 8 * p.a, lo);
+            if (p.b >= 0) store8(to + 8 * p.b, hi);
         }
     }
     if (!a.grad_q_weight && !a.grad_k_weight) return;
     // sums over the workgroup's heads, queries and keys apart, in their order
-    const int slot = threadIdx.x / LANES;
+    const int slot = threadIdx.x / LANES, slots = blockDim.x / LANES;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (p.a >= 0) sums[slot * WIDE + 8 * p.a + i] = gw[i];
@@ -251,12 +272,14 @@ __global__ __launch_bounds__(kThreads) void head_rope_bwd_kernel(DsqRopeBwdArgs 
     }
     __syncthreads();
     float *to = a.partial + (int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.dim;
-    const int first = blockIdx.y * HEADS;
-    for (int i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
+    const int first = blockIdx.y * share.heads, used = share.heads * share.rows < slots ? share.heads * share.rows : slots;
+    for (int i = threadIdx.x; i < 2 * a.dim; i += blockDim.x) {
         const int d = i % a.dim, begin = i < a.dim ? 0 : a.q_heads, end = i < a.dim ? a.q_heads : units;
         float s = 0.0f;
-        for (int u = 0; u < HEADS; ++u)
-            if (first + u >= begin && first + u < end) s += sums[u * WIDE + d];
+        for (int u = 0; u < used; ++u) {
+            const int unit = first + u % share.heads;
+            if (unit >= begin && unit < end) s += sums[u * WIDE + d];
+        }
         to[i] = s;
     }
 }
@@ -268,6 +291,7 @@ __global__ __launch_bounds__(1024) void head_rope_gw_kernel(const float *partial
     const int column = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
     double s = 0.0;
     if (column < 2 * dim)
+#pragma unroll 8
         for (int i = part; i < parts; i += 64) s += (double)partial[(int64_t)i * 2 * dim + column];
     sums[part][threadIdx.x % 16] = s;
     __syncthreads();
@@ -278,29 +302,41 @@ __global__ __launch_bounds__(1024) void head_rope_gw_kernel(const float *partial
 }
 
 int lanes_of(int dim) { return dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16; }
-int blocks_of(int units, int dim) { return (units * lanes_of(dim) + kThreads - 1) / kThreads; }
-// Workgroups of the backward pass along the rows: four a compute unit.
-int row_groups(int rows, int blocks)
+// Several rows of few heads, or part of a row of more than 256 threads' worth; whole waves.
+Share share_of(int rows, int units, int dim)
 {
-    const int most = 1024 / blocks > 1 ? 1024 / blocks : 1;
-    return rows < most ? rows : most;
+    const int lanes = lanes_of(dim), row = units * lanes;
+    Share s;
+    s.blocks = (row + kThreads - 1) / kThreads;
+    s.heads = (units + s.blocks - 1) / s.blocks;
+    s.rows = s.blocks > 1 ? 1 : 256 / row < 1 ? 1 : 256 / row < kRows ? 256 / row : kRows;
+    if (s.rows > rows) s.rows = rows;
+    s.threads = (s.rows * s.heads * lanes + 63) / 64 * 64;
+    return s;
+}
+// Workgroups of the backward pass along the rows: three a compute unit, as many as its registers hold (four take a third longer).
+int row_groups(int rows, const Share &s)
+{
+    const int groups = (rows + s.rows - 1) / s.rows, most = 768 / s.blocks > 1 ? 768 / s.blocks : 1;
+    return groups < most ? groups : most;
 }
 
 template <class E, int LANES>
 hipError_t forward(const DsqRopeArgs &a, hipStream_t stream)
 {
-    const int units = a.q_heads + a.kv_heads + (a.cache.k ? a.kv_heads : 0);
-    head_rope_kernel<E, LANES><<<dim3(a.rows, blocks_of(units, a.dim)), kThreads, 0, stream>>>(a);
+    const Share s = share_of(a.rows, a.q_heads + a.kv_heads + (a.cache.k ? a.kv_heads : 0), a.dim);
+    head_rope_kernel<E, LANES><<<dim3((a.rows + s.rows - 1) / s.rows, s.blocks), s.threads, 0, stream>>>(a, s);
     return hipGetLastError();
 }
 template <class E, int LANES>
 hipError_t backward(const DsqRopeBwdArgs &a, hipStream_t stream)
 {
-    const int blocks = blocks_of(a.q_heads + a.kv_heads, a.dim), groups = row_groups(a.rows, blocks);
-    head_rope_bwd_kernel<E, LANES><<<dim3(groups, blocks), kThreads, 0, stream>>>(a);
+    const Share s = share_of(a.rows, a.q_heads + a.kv_heads, a.dim);
+    const int groups = row_groups(a.rows, s);
+    head_rope_bwd_kernel<E, LANES><<<dim3(groups, s.blocks), s.threads, 0, stream>>>(a, s);
     if (const hipError_t e = hipGetLastError()) return e;
     if (a.grad_q_weight || a.grad_k_weight)
-        head_rope_gw_kernel<<<(2 * a.dim + 15) / 16, 1024, 0, stream>>>(a.partial, a.grad_q_weight, a.grad_k_weight, groups * blocks, a.dim);
+        head_rope_gw_kernel<<<(2 * a.dim + 15) / 16, 1024, 0, stream>>>(a.partial, a.grad_q_weight, a.grad_k_weight, groups * s.blocks, a.dim);
     return hipGetLastError();
 }
 
@@ -339,8 +375,8 @@ hipError_t of_type(const A &a, int type, hipStream_t stream)
 
 int dsq_rope_bwd_parts(int rows, int q_heads, int kv_heads, int dim)
 {
-    const int blocks = blocks_of(q_heads + kv_heads, dim);
-    return row_groups(rows, blocks) * blocks;
+    const Share s = share_of(rows, q_heads + kv_heads, dim);
+    return row_groups(rows, s) * s.blocks;
 }
 hipError_t dsq_launch_qk_norm_rope(const DsqRopeArgs &a, int type, hipStream_t stream) { return of_type(a, type, stream); }
 hipError_t dsq_launch_qk_norm_rope_bwd(const DsqRopeBwdArgs &a, int type, hipStream_t stream) { return of_type(a, type, stream); }
