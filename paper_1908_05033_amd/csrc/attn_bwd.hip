@@ -49,7 +49,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
 {
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KEYS = 32 * SPLIT, STEPS = HD / 16, DT = HD / 32, BUFFERS = SPLIT == 1 ? 2 : 1;
+    constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 ? 2 : 1, KEYS = 32 * KT * SPLIT, STEPS = HD / 16, DT = HD / 32;
+    constexpr int BUFFERS = SPLIT == 1 ? 2 : 1;
     constexpr int TILE = KEYS * HD, JOIN = (SPLIT - 1) * ROW_WAVES * DT * 4096;
     __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
     E *const tiles_at = reinterpret_cast<E *>(room);
@@ -99,8 +100,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
         km.fetch(kp, a.k.row, 0, k_end, a.dim);
         vm.fetch(vp, a.v.row, 0, k_end, a.dim);
     }
-    for (int t = 0; t < count; ++t) {
-        E *const kt = tiles_at + (BUFFERS == 2 ? t & 1 : 0) * 2 * TILE, *const vt = kt + TILE;
+    const auto block = [&](int t, auto buffer) {
+        E *const kt = tiles_at + decltype(buffer)::value * 2 * TILE, *const vt = kt + TILE;
         if (BUFFERS == 1) __syncthreads();
         km.put(kt);
         vm.put(vt);
@@ -109,13 +110,16 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
             km.fetch(kp, a.k.row, (t + 1) * KEYS, k_end, a.dim);
             vm.fetch(vp, a.v.row, (t + 1) * KEYS, k_end, a.dim);
         }
-        const int at = t * KEYS + part * 32;                     // the wave's first key
-        if (at < any) {
+#pragma unroll
+        for (int n = 0; n < KT; ++n) {
+            const int in = (part * KT + n) * 32, at = t * KEYS + in;     // the wave's first key, and its place in the tile
+            if (at >= any) break;
             v16f x = zeros(), y = zeros();
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::row_operand(kt, part * 32 + r, i, h), q[i], x);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) y = multiply(T::row_operand(vt, part * 32 + r, i, h), g[i], y);
+            for (int i = 0; i < STEPS; ++i) {
+                x = multiply(T::row_operand(kt, in + r, i, h), q[i], x);
+                y = multiply(T::row_operand(vt, in + r, i, h), g[i], y);
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse));
@@ -131,9 +135,13 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
             for (int half = 0; half < 2; ++half) {
                 const V8 ds = operand_of<E>(x, half);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) dq[d] = multiply(T::column_operand(kt, part * 32 + half * 16, d * 32, lane), ds, dq[d]);
+                for (int d = 0; d < DT; ++d) dq[d] = multiply(T::column_operand(kt, in + half * 16, d * 32, lane), ds, dq[d]);
             }
         }
+    };
+    for (int t = 0; t < count; t += 2) {
+        block(t, std::integral_constant<int, 0>());
+        if (t + 1 < count) block(t + 1, std::integral_constant<int, BUFFERS - 1>());
     }
     join<DT>(dq, reinterpret_cast<float *>(room), wave % ROW_WAVES, ROW_WAVES, part, SPLIT, lane);
     if (there && part == 0) store_row<E, DT>((E *)a.grad_q.p + token * a.grad_q.row + head * a.grad_q.head, dq, a.scale, h, a.dim);
@@ -306,7 +314,16 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(DsqAttnBwdArgs a, in
     }
 }
 
-constexpr int64_t kFew = 256 * 128;
+// Rows times heads up to which the waves of the queries' kernel split the keys.  Both kernels together, us, 128 (binary32: 64) rows / 32
+// rows a workgroup:
+//
+//                   1024 x 8    2048 x 8    1024 x 32   2048 x 16   4096 x 8
+//   bfloat16, 128   76 / 59     119 / 92    91 / 111    131 / 147   232 / 238
+//   bfloat16, 64    54 / 41     85 / 59     62 / 59     91 / 77     162 / 124
+//   binary32, 128   190 / 142   402 / 330   335 / 380   603 / 653   1136 / 1200
+template <class E, int HD>
+constexpr int64_t kFew = sizeof(E) == 2 && HD == 64 ? 49152 : 32768;
+
 
 int tiles_of(const DsqAttnBwdArgs &a, int rows, int tile) { return a.q_starts ? rows / tile + a.sequences : (rows + tile - 1) / tile; }
 
@@ -339,7 +356,7 @@ hipError_t launch(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     constexpr bool SINGLE = sizeof(E) == 4;
     if (a.q_rows > 0)
-        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew ? queries<E, HD, 1>(a, stream) : queries<E, HD, SINGLE ? 2 : 4>(a, stream)) return e;
+        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew<E, HD> ? queries<E, HD, 1>(a, stream) : queries<E, HD, SINGLE ? 2 : 4>(a, stream)) return e;
     return a.k_rows > 0 ? keys<E, HD, SINGLE ? 1 : 2, 2, 2>(a, stream) : hipSuccess;
 }
 

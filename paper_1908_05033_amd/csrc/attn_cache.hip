@@ -256,7 +256,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
             next = j + 2 * STRIDE < w.end ? pages.row(j + 2 * STRIDE + r) : -1;
         }
         any |= mask;
-        attend<E, HD, 1>(ks, vs, 0, q, c, m, l, o, [&](v16f (&x)[1]) { hide_keys(x[0], mask, h); });
+        attend<E, HD, 1>(ks, vs, 0, q, c, m, l, o, lane, [&](v16f (&x)[1]) { hide_keys(x[0], mask, h); });
         wave_order();
     }
 
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
 #pragma unroll
         for (int n = 0; n < KT; ++n) any |= mask[n];
         if (busy)
-            attend<E, HD, KT>(kt, vt, 0, q, c, m, l, o, [&](v16f (&x)[KT]) {
+            attend<E, HD, KT>(kt, vt, 0, q, c, m, l, o, lane, [&](v16f (&x)[KT]) {
 #pragma unroll
                 for (int n = 0; n < KT; ++n) hide_keys(x[n], mask[n], h);
             });

@@ -288,10 +288,10 @@ constexpr float kNoKey = -3.0e38f;
 // base 2) of the lane's row and the transposed sums o.  `hide` puts -inf in the place of scores that are not seen.
 template <class E, int HD, int KT, class Hide>
 __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[HD / 16], float c, float &m, float &l,
-                                       v16f (&o)[HD / 32], Hide hide)
+                                       v16f (&o)[HD / 32], int lane, Hide hide)
 {
     typedef Tile<E, HD> T;
-    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const int r = lane & 31, h = lane >> 5;
     v16f x[KT];
 #pragma unroll
     for (int n = 0; n < KT; ++n) {

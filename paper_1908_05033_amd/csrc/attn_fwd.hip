@@ -21,7 +21,15 @@ struct Fwd {
     typedef Tile<E, HD> T;
 };
 
-constexpr int64_t kFew = 256 * 128;
+// Rows times heads up to which waves split the keys: there 128 rows a workgroup leave compute units idle and make few long walks over the
+// keys.  Us, 128 rows / 32 rows a workgroup, rows x heads (causal):
+//
+//                   1024 x 8   2048 x 8   1024 x 32   2048 x 16   4096 x 8
+//   bfloat16, 128   26 / 20    46 / 40    28 / 54     48 / 78     88 / 127
+//   bfloat16, 64    18 / 12    31 / 20    19 / 21     32 / 31     58 / 49
+//   binary32, 128   144 / 58   283 / 123  146 / 146   284 / 246   559 / 444
+template <class E, int HD>
+constexpr int64_t kFew = sizeof(E) == 2 && HD == 128 ? 32768 : 49152;
 
 // Keys of one row of a packed prompt.
 template <class E>
@@ -89,7 +97,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64)
         if (t + 1 < count) fetch(t + 1);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
         if (at < any)
-            attend<E, HD, F::KT>(kt, vt, in, q, c, m, l, o, [&](v16f (&x)[F::KT]) {
+            attend<E, HD, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) {
                 if (at + 32 * F::KT <= whole) return;
                 stay_a_branch();
                 const int left = seen - at - 4 * h;
@@ -173,7 +181,7 @@ hipError_t launch(const DsqAttnArgs &a, hipStream_t stream)
 template <class E, int HD>
 hipError_t of_rows(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return (int64_t)a.q_rows * a.q_heads < kFew ? launch<E, HD, 1>(a, stream) : launch<E, HD, 4>(a, stream);
+    return (int64_t)a.q_rows * a.q_heads < kFew<E, HD> ? launch<E, HD, 1>(a, stream) : launch<E, HD, 4>(a, stream);
 }
 
 template <class E>
