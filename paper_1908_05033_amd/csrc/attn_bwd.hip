@@ -53,6 +53,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     constexpr int BUFFERS = SPLIT == 1 ? 2 : 1;
     constexpr int TILE = KEYS * HD, JOIN = (SPLIT - 1) * ROW_WAVES * DT * 4096;
     __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
+    __shared__ float parts[SPLIT][ROWS];
     E *const tiles_at = reinterpret_cast<E *>(room);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5, part = wave / ROW_WAVES;
@@ -83,10 +84,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     }
     delta = both_sum(delta);
     const int64_t stat = (int64_t)head * a.q_rows + token;
-    if (there && h == 0 && part == 0) a.delta[stat] = delta;
     const int seen = there ? visible(s, a.causal, row) : 0;
     const float lse = seen > 0 ? a.lse[stat] * kLog2e - kLift<E> : 0.0f;
-    delta *= kDrop<E>;
     const int last_row = first_row + 31 < s.q_len ? first_row + 31 : s.q_len - 1;
     const int whole = first_row + 31 < s.q_len ? visible(s, a.causal, first_row) : 0;
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
@@ -100,6 +99,60 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
         km.fetch(kp, a.k.row, 0, k_end, a.dim);
         vm.fetch(vp, a.v.row, 0, k_end, a.dim);
     }
+    // One block of keys, in a buffer whose place the compiler knows: p in x, grad_out . v in y, zeros for what is not seen.
+    const auto scores = [&](const E *kt, const E *vt, int in, int at, v16f &x, v16f &y) {
+        x = y = zeros();
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            x = multiply(T::row_operand(kt, in + r, i, h), q[i], x);
+            y = multiply(T::row_operand(vt, in + r, i, h), g[i], y);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse));
+        if (at + 32 > whole) {
+            stay_a_branch();
+            const int left = seen - at - 4 * h;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
+                y[i] = 8 * (i / 4) + i % 4 < left ? y[i] : 0.0f;
+            }
+        }
+    };
+    // D is formed from the result as it was stored.  Rows of few keys have large results, whose rounding is a third of the error of all gradients
+    // together: they form it again from p.
+    if (sizeof(E) == 2 && k_end <= 128) {
+        float sum = 0.0f;
+        for (int t = 0; t < count; ++t) {
+            __syncthreads();
+            km.put(tiles_at);
+            vm.put(tiles_at + TILE);
+            __syncthreads();
+            const int next = t + 1 < count ? t + 1 : 0;
+            km.fetch(kp, a.k.row, next * KEYS, k_end, a.dim);
+            vm.fetch(vp, a.v.row, next * KEYS, k_end, a.dim);
+            for (int n = 0; n < KT; ++n) {
+                const int in = (part * KT + n) * 32, at = t * KEYS + in;
+                if (at >= any) break;
+                v16f x, y;
+                scores(tiles_at, tiles_at + TILE, in, at, x, y);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(x[i], y[i], sum);
+            }
+        }
+        sum = both_sum(sum) * kDrop<E>;
+        if (SPLIT > 1) {
+            if (h == 0) parts[part][wave % ROW_WAVES * 32 + r] = sum;
+            __syncthreads();
+            sum = 0.0f;
+#pragma unroll
+            for (int p = 0; p < SPLIT; ++p) sum += parts[p][wave % ROW_WAVES * 32 + r];
+        }
+        __syncthreads();
+        delta = sum;
+    }
+    if (there && h == 0 && part == 0) a.delta[stat] = delta;
+    delta *= kDrop<E>;
     const auto block = [&](int t, auto buffer) {
         E *const kt = tiles_at + decltype(buffer)::value * 2 * TILE, *const vt = kt + TILE;
         if (BUFFERS == 1) __syncthreads();
@@ -114,23 +167,10 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
         for (int n = 0; n < KT; ++n) {
             const int in = (part * KT + n) * 32, at = t * KEYS + in;     // the wave's first key, and its place in the tile
             if (at >= any) break;
-            v16f x = zeros(), y = zeros();
+            v16f x, y;
+            scores(kt, vt, in, at, x, y);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                x = multiply(T::row_operand(kt, in + r, i, h), q[i], x);
-                y = multiply(T::row_operand(vt, in + r, i, h), g[i], y);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse));
-                x[i] = p * __builtin_fmaf(y[i], kDrop<E>, -delta);
-            }
-            if (at + 32 > whole) {
-                stay_a_branch();
-                const int left = seen - at - 4 * h;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
-            }
+            for (int i = 0; i < 16; ++i) x[i] *= __builtin_fmaf(y[i], kDrop<E>, -delta);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const V8 ds = operand_of<E>(x, half);
