@@ -44,12 +44,13 @@ __device__ __forceinline__ void store_row(E *to, const v16f (&o)[DT], float by, 
 //
 // ROW_WAVES waves own 32 rows each; the others take other blocks of 32 keys for the same rows, and their sums are joined.
 
-template <class E, int HD, int ROW_WAVES>
+template <class E, int WIDTH, int ROW_WAVES>
 __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void attn_bwd_q_kernel(DsqAttnBwdArgs a, int tiles)
 {
+    constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32;
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 ? 2 : 1, KEYS = 32 * KT * SPLIT, STEPS = HD / 16, DT = HD / 32;
+    constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 ? 2 : 1, KEYS = 32 * KT * SPLIT;
     constexpr int BUFFERS = SPLIT == 1 ? 2 : 1;
     constexpr int TILE = KEYS * HD, JOIN = (SPLIT - 1) * ROW_WAVES * DT * 4096;
     __shared__ __align__(16) char room[most(BUFFERS * 2 * TILE * (int)sizeof(E), JOIN)];
@@ -199,13 +200,14 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
 // one wave holds both sums and operands, one wave a SIMD, 422; one block of rows at a time 234; pairs 2 x 1 or 1 x 2, two workgroups
 // a compute unit, 350 and 284.)
 
-template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS, int SUB>
+template <class E, int WIDTH, int KEY_PAIRS, int ROW_PAIRS, int SUB>
 __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS == 4 ? 2 : 1) void attn_bwd_k_kernel(DsqAttnBwdArgs a, int tiles, int splits)
 {
+    constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32;
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
     constexpr int PAIRS = KEY_PAIRS * ROW_PAIRS, THREADS = 128 * PAIRS, KEYS = 32 * KEY_PAIRS, MINE = 32 * SUB, ROWS = MINE * ROW_PAIRS;
-    constexpr int STEPS = HD / 16, DT = HD / 32, TILE = ROWS * HD, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
+    constexpr int TILE = ROWS * HD, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
     __shared__ __align__(16) char room[most(2 * TILE * (int)sizeof(E), JOIN)];
     __shared__ __align__(16) float handed[PAIRS][SUB][16 * 64], stats[2][ROWS];
 
@@ -361,20 +363,20 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(DsqAttnBwdArgs a, in
 //   bfloat16, 128   76 / 59     119 / 92    91 / 111    131 / 147   232 / 238
 //   bfloat16, 64    54 / 41     85 / 59     62 / 59     91 / 77     162 / 124
 //   binary32, 128   190 / 142   402 / 330   335 / 380   603 / 653   1136 / 1200
-template <class E, int HD>
-constexpr int64_t kFew = sizeof(E) == 2 && HD == 64 ? 49152 : 32768;
+template <class E, int WIDTH>
+constexpr int64_t kFew = sizeof(E) == 2 && WIDTH == 64 ? 49152 : 32768;
 
 
 int tiles_of(const DsqAttnBwdArgs &a, int rows, int tile) { return a.q_starts ? rows / tile + a.sequences : (rows + tile - 1) / tile; }
 
-template <class E, int HD, int ROW_WAVES>
+template <class E, int WIDTH, int ROW_WAVES>
 hipError_t queries(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     const int tiles = tiles_of(a, a.q_rows, 32 * ROW_WAVES);
-    attn_bwd_q_kernel<E, HD, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    attn_bwd_q_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
-template <class E, int HD, int KEY_PAIRS, int ROW_PAIRS, int SUB>
+template <class E, int WIDTH, int KEY_PAIRS, int ROW_PAIRS, int SUB>
 hipError_t keys(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     const int tiles = tiles_of(a, a.k_rows, 32 * KEY_PAIRS);
@@ -384,26 +386,26 @@ hipError_t keys(const DsqAttnBwdArgs &a, hipStream_t stream)
     const int64_t blocks = (a.q_rows / (32 * SUB * ROW_PAIRS) + 1LL) * (a.q_heads / a.kv_heads), room = (int64_t)(a.partial_bytes / 8) / each;
     for (const int64_t limit : {blocks, room, (int64_t)16}) splits = splits < limit ? splits : limit;
     splits = splits < 1 ? 1 : splits;
-    attn_bwd_k_kernel<E, HD, KEY_PAIRS, ROW_PAIRS, SUB>
+    attn_bwd_k_kernel<E, WIDTH, KEY_PAIRS, ROW_PAIRS, SUB>
         <<<(unsigned)((groups * splits + 7) / 8 * 8), 128 * KEY_PAIRS * ROW_PAIRS, 0, stream>>>(a, tiles, (int)splits);
     if (const hipError_t e = hipGetLastError()) return e;
     if (splits > 1) attn_bwd_join_kernel<E><<<(unsigned)((each / 4 + 255) / 256), 256, 0, stream>>>(a, (int)splits);
     return hipGetLastError();
 }
 
-template <class E, int HD>
+template <class E, int WIDTH>
 hipError_t launch(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     constexpr bool SINGLE = sizeof(E) == 4;
     if (a.q_rows > 0)
-        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew<E, HD> ? queries<E, HD, 1>(a, stream) : queries<E, HD, SINGLE ? 2 : 4>(a, stream)) return e;
-    return a.k_rows > 0 ? keys<E, HD, SINGLE ? 1 : 2, 2, 2>(a, stream) : hipSuccess;
+        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew<E, WIDTH> ? queries<E, WIDTH, 1>(a, stream) : queries<E, WIDTH, SINGLE ? 2 : 4>(a, stream)) return e;
+    return a.k_rows > 0 ? keys<E, WIDTH, SINGLE ? 1 : 2, 2, 2>(a, stream) : hipSuccess;
 }
 
 template <class E>
 hipError_t of_dim(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? launch<E, 64>(a, stream) : launch<E, 128>(a, stream);
+    return a.dim <= 64 ? launch<E, 64>(a, stream) : a.dim <= 96 ? launch<E, 96>(a, stream) : launch<E, 128>(a, stream);
 }
 
 }  // namespace

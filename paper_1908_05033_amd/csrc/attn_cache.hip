@@ -190,13 +190,14 @@ __device__ __forceinline__ void hide_keys(v16f &x, uint32_t mask, int h)
 
 // ---- up to 32 rows: WAVES waves take blocks of 32 keys in turn ------------------------------------------
 
-template <class E, int HD, int WAVES>
+template <class E, int WIDTH, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache_kernel(DsqAttnCacheArgs a, int slots)
 {
+    constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32;
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int STEPS = HD / 16, DT = HD / 32, PIECES = 32 * T::UNITS / 64, PITCH = 33, STRIDE = 32 * WAVES;
-    constexpr int WAVE_BYTES = most(HD * PITCH * 4, 64 * HD * (int)sizeof(E));
+    constexpr int PIECES = 32 * T::UNITS / 64, PITCH = 33, STRIDE = 32 * WAVES;
+    constexpr int WAVE_BYTES = most(WIDTH * PITCH * 4, 64 * HD * (int)sizeof(E));
     __shared__ __align__(16) char room[WAVES * WAVE_BYTES];
     __shared__ float stat[WAVES][2][32];
     __shared__ uint32_t seen_by[WAVES][32];
@@ -256,11 +257,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
             next = j + 2 * STRIDE < w.end ? pages.row(j + 2 * STRIDE + r) : -1;
         }
         any |= mask;
-        attend<E, HD, 1>(ks, vs, 0, q, c, m, l, o, lane, [&](v16f (&x)[1]) { hide_keys(x[0], mask, h); });
+        attend<E, WIDTH, 1>(ks, vs, 0, q, c, m, l, o, lane, [&](v16f (&x)[1]) { hide_keys(x[0], mask, h); });
         wave_order();
     }
 
-    // ---- the waves' rows: [HD][PITCH] of each in the room of its tiles
+    // ---- the waves' rows: [WIDTH][PITCH] of each in the room of its tiles
     float *mine_o = reinterpret_cast<float *>(room + wave * WAVE_BYTES);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
         for (int e = 0; e < 2; ++e) {
             const int d = lane + 64 * e;
             y[e] = 0.0f;
-            if (d < HD) {
+            if (d < WIDTH) {
 #pragma unroll
                 for (int v = 0; v < WAVES; ++v)
                     y[e] = __builtin_fmaf(reinterpret_cast<const float *>(room + v * WAVE_BYTES)[d * PITCH + i], f[v], y[e]);
@@ -306,12 +307,13 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
 
 // ---- more rows: four waves take 32 each, over tiles of keys that they share ------------------------------------
 
-template <class E, int HD>
+template <class E, int WIDTH>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_kernel(DsqAttnCacheArgs a, int slots, int row_tiles)
 {
+    constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32;
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int STEPS = HD / 16, DT = HD / 32, KT = sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT, TILE = KEYS * HD;
+    constexpr int KT = sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT, TILE = KEYS * HD;
     constexpr int PIECES = KEYS * T::UNITS / 256, STEP = 256 / T::UNITS;
     __shared__ __align__(16) E tiles_at[2][2][TILE];
     __shared__ uint32_t there_at[2][KT];
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
 #pragma unroll
         for (int n = 0; n < KT; ++n) any |= mask[n];
         if (busy)
-            attend<E, HD, KT>(kt, vt, 0, q, c, m, l, o, lane, [&](v16f (&x)[KT]) {
+            attend<E, WIDTH, KT>(kt, vt, 0, q, c, m, l, o, lane, [&](v16f (&x)[KT]) {
 #pragma unroll
                 for (int n = 0; n < KT; ++n) hide_keys(x[n], mask[n], h);
             });
@@ -550,14 +552,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
     }
 }
 
-template <class E, int HD>
+template <class E, int WIDTH>
 hipError_t launch(const DsqAttnCacheArgs &a, hipStream_t stream)
 {
     const AttnCachePlan p = attn_cache_plan(a.max_rows, a.q_heads, a.kv_heads, a.sequences, (int64_t)a.table_pages << a.page_bits);
     const unsigned groups = (unsigned)((int64_t)(p.slots + a.sequences) * p.row_tiles * a.kv_heads);
-    if (p.tiles) attn_cache_tiles_kernel<E, HD><<<groups, 256, 0, stream>>>(a, p.slots, p.row_tiles);
-    else if (p.single) attn_cache_kernel<E, HD, sizeof(E) == 2 ? 8 : 4><<<groups, sizeof(E) == 2 ? 512 : 256, 0, stream>>>(a, p.slots);
-    else attn_cache_kernel<E, HD, 4><<<groups, 256, 0, stream>>>(a, p.slots);
+    if (p.tiles) attn_cache_tiles_kernel<E, WIDTH><<<groups, 256, 0, stream>>>(a, p.slots, p.row_tiles);
+    else if (p.single) attn_cache_kernel<E, WIDTH, sizeof(E) == 2 ? 8 : 4><<<groups, sizeof(E) == 2 ? 512 : 256, 0, stream>>>(a, p.slots);
+    else attn_cache_kernel<E, WIDTH, 4><<<groups, 256, 0, stream>>>(a, p.slots);
     if (const hipError_t e = hipGetLastError()) return e;
     if (p.single) return hipSuccess;
     // Many chunks a row: a workgroup of 16 waves each; a few: a wave takes one row, or four where there are many.
@@ -571,7 +573,7 @@ hipError_t launch(const DsqAttnCacheArgs &a, hipStream_t stream)
 template <class E>
 hipError_t of_dim(const DsqAttnCacheArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? launch<E, 64>(a, stream) : launch<E, 128>(a, stream);
+    return a.dim <= 64 ? launch<E, 64>(a, stream) : a.dim <= 96 ? launch<E, 96>(a, stream) : launch<E, 128>(a, stream);
 }
 
 }  // namespace

@@ -139,6 +139,10 @@ struct Mover {
 // Keeps the compiler from computing a rarely taken branch's selections always.
 __device__ __forceinline__ void stay_a_branch() { asm volatile(""); }
 
+// Heads of up to 64, 96 and 128 elements have kernels of their own (WIDTH); rows of a tile have 64 or 128.
+template <int WIDTH>
+constexpr int kRow = WIDTH == 64 ? 64 : 128;
+
 // The wave's number within its workgroup, known to the compiler to be the same for all lanes.
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
@@ -286,18 +290,18 @@ constexpr float kNoKey = -3.0e38f;
 //
 // 32 KT keys, from row `in` of the tiles kt and vt on, for the 32 rows of a wave: running maximum m and sum l (of the scores times c, to
 // base 2) of the lane's row and the transposed sums o.  `hide` puts -inf in the place of scores that are not seen.
-template <class E, int HD, int KT, class Hide>
-__device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[HD / 16], float c, float &m, float &l,
-                                       v16f (&o)[HD / 32], int lane, Hide hide)
+template <class E, int WIDTH, int KT, class Hide>
+__device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[WIDTH / 16], float c, float &m, float &l,
+                                       v16f (&o)[WIDTH / 32], int lane, Hide hide)
 {
-    typedef Tile<E, HD> T;
+    typedef Tile<E, kRow<WIDTH>> T;
     const int r = lane & 31, h = lane >> 5;
     v16f x[KT];
 #pragma unroll
     for (int n = 0; n < KT; ++n) {
         x[n] = zeros();
 #pragma unroll
-        for (int i = 0; i < HD / 16; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
+        for (int i = 0; i < WIDTH / 16; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
     }
     hide(x);
     float most = x[0][0];
@@ -312,7 +316,7 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
         m = next;
         l *= f;
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d)
+        for (int d = 0; d < WIDTH / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] *= f;
     }
@@ -329,7 +333,7 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
         for (int half = 0; half < 2; ++half) {
             const typename Operand<E>::type p = operand_of<E>(x[n], half);
 #pragma unroll
-            for (int d = 0; d < HD / 32; ++d) o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
+            for (int d = 0; d < WIDTH / 32; ++d) o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
         }
 }
 

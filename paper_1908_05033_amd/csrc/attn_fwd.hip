@@ -13,10 +13,10 @@
 namespace {
 
 // ROW_WAVES waves own 32 rows each; the others take other blocks of keys for the same rows, and their sums are joined at the end.
-template <class E, int HD, int ROW_WAVES>
+template <class E, int WIDTH, int ROW_WAVES>
 struct Fwd {
     static constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 && sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT * SPLIT;
-    static constexpr int STEPS = HD / 16, DT = HD / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
+    static constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
     static constexpr int BYTES = most(BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
     typedef Tile<E, HD> T;
 };
@@ -28,8 +28,8 @@ struct Fwd {
 //   bfloat16, 128   26 / 20    46 / 40    28 / 54     48 / 78     88 / 127
 //   bfloat16, 64    18 / 12    31 / 20    19 / 21     32 / 31     58 / 49
 //   binary32, 128   144 / 58   283 / 123  146 / 146   284 / 246   559 / 444
-template <class E, int HD>
-constexpr int64_t kFew = sizeof(E) == 2 && HD == 128 ? 32768 : 49152;
+template <class E, int WIDTH>
+constexpr int64_t kFew = sizeof(E) == 2 && WIDTH > 64 ? 32768 : 49152;
 
 // Keys of one row of a packed prompt.
 template <class E>
@@ -43,10 +43,10 @@ struct PromptKeys {
     __device__ const E *value(int j) const { return v + j * v_row; }
 };
 
-template <class E, int HD, int ROW_WAVES>
-__global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64) ? 2 : 1) void attn_fwd_kernel(DsqAttnArgs a, int tiles)
+template <class E, int WIDTH, int ROW_WAVES>
+__global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 64) ? 2 : 1) void attn_fwd_kernel(DsqAttnArgs a, int tiles)
 {
-    typedef Fwd<E, HD, ROW_WAVES> F;
+    typedef Fwd<E, WIDTH, ROW_WAVES> F;
     typedef typename F::T T;
     typedef typename Operand<E>::type V8;
     __shared__ __align__(16) char room[F::BYTES];
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64)
     const int whole = first_row + 31 < s.q_len ? visible(s, a.causal, first_row) : 0;
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
 
-    Mover<E, HD, F::KEYS> km, vm;
+    Mover<E, F::HD, F::KEYS> km, vm;
     auto fetch = [&](int t) {
         km.fetch(kp, a.k.row, t * F::KEYS, k_end, a.dim);
         vm.fetch(vp, a.v.row, t * F::KEYS, k_end, a.dim);
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64)
         if (t + 1 < count) fetch(t + 1);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
         if (at < any)
-            attend<E, HD, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) {
+            attend<E, WIDTH, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) {
                 if (at + 32 * F::KT <= whole) return;
                 stay_a_branch();
                 const int left = seen - at - 4 * h;
@@ -170,24 +170,24 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || HD == 64)
     }
 }
 
-template <class E, int HD, int ROW_WAVES>
+template <class E, int WIDTH, int ROW_WAVES>
 hipError_t launch(const DsqAttnArgs &a, hipStream_t stream)
 {
-    const int rows = Fwd<E, HD, ROW_WAVES>::ROWS, tiles = a.q_starts ? a.q_rows / rows + a.sequences : (a.q_rows + rows - 1) / rows;
-    attn_fwd_kernel<E, HD, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    const int rows = Fwd<E, WIDTH, ROW_WAVES>::ROWS, tiles = a.q_starts ? a.q_rows / rows + a.sequences : (a.q_rows + rows - 1) / rows;
+    attn_fwd_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 
-template <class E, int HD>
+template <class E, int WIDTH>
 hipError_t of_rows(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return (int64_t)a.q_rows * a.q_heads < kFew<E, HD> ? launch<E, HD, 1>(a, stream) : launch<E, HD, 4>(a, stream);
+    return (int64_t)a.q_rows * a.q_heads < kFew<E, WIDTH> ? launch<E, WIDTH, 1>(a, stream) : launch<E, WIDTH, 4>(a, stream);
 }
 
 template <class E>
 hipError_t of_dim(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? of_rows<E, 64>(a, stream) : of_rows<E, 128>(a, stream);
+    return a.dim <= 64 ? of_rows<E, 64>(a, stream) : a.dim <= 96 ? of_rows<E, 96>(a, stream) : of_rows<E, 128>(a, stream);
 }
 
 }  // namespace

@@ -11,7 +11,7 @@ FULL = ("attn_fwd_kernelIDF16_Li128ELi4E", "attn_fwd_kernelIDF16bLi128ELi4E", "a
         "attn_bwd_q_kernelIfLi128ELi1E")
 
 
-@pytest.mark.parametrize("source,count", [("head_rope.hip", 31), ("attn_fwd.hip", 12), ("attn_bwd.hip", 21), ("attn_cache.hip", 25)])
+@pytest.mark.parametrize("source,count", [("head_rope.hip", 31), ("attn_fwd.hip", 18), ("attn_bwd.hip", 30), ("attn_cache.hip", 33)])
 def test_kernels_stay_inside_their_registers(source, count):
     asm = _device_asm(os.path.join(CSRC, source))
     kernels = re.findall(r"\.name:\s+(\S+).*?\.private_segment_fixed_size:\s+(\d+).*?\.vgpr_count:\s+(\d+).*?\.vgpr_spill_count:\s+(\d+)", asm, re.S)
