@@ -518,6 +518,7 @@ dsq_status dsq_linear_w4a8(const int8_t *codes, size_t codes_bytes,
  *   as the nearest end.
  *   A paged cache is two tensors [pages][kv_heads][page][dim], keys and values; page is a power
  *   of two up to 2^16.
+ *   Outputs overlap neither inputs nor each other where a call does not say so.
  *   Sums, softmax and products are binary32; probabilities (and in the backward pass ds) are rounded
  *   to dtype where they meet values in the matrix instruction.
  */
@@ -651,7 +652,8 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
  *            not seen; or NULL
  * workspace  device, dsq_attention_cache_bytes(..) bytes; of no other call that may run at the same
  *            time, captured graphs included
- * A sequence has at most 2^30 keys (table_pages * page).
+ * A sequence has at most 2^30 keys (table_pages * page), all sequences together 2^37 by their tables, and
+ * max_rows times the heads that share a key head are at most 2^30 (DSQ_ERR_UNSUPPORTED).
  */
 dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head,
                                dsq_dtype dtype, int rows, int q_heads, int kv_heads,

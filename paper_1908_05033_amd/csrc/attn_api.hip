@@ -267,7 +267,7 @@ dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head, dsq
     if (rows == 0 || sequences == 0) return DSQ_OK;
     const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads, sequences, (int64_t)table_pages << bits);
     if ((int64_t)(p.slots + sequences) * p.row_tiles * kv_heads > 0x7fffffff || (int64_t)rows * q_heads > 0x7fffffff ||
-        (((int64_t)table_pages << bits) / 128 + 1) * sequences > 0x7fffffff)
+        (((int64_t)table_pages << bits) / 128 + 1) * sequences > 1 << 30 || (int64_t)max_rows * (q_heads / kv_heads) > 1 << 30)
         return DSQ_ERR_UNSUPPORTED;
     if (!q || !out || !lengths || !workspace || (pages && (!k_cache || !v_cache)) || (table_pages && !page_table)) return DSQ_ERR_NULL;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_starts) || !aligned16(page_table) || !aligned16(lengths) ||

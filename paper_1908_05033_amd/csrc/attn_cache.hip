@@ -58,6 +58,9 @@ __device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int slots,
     return __builtin_amdgcn_readfirstlane(at);
 }
 
+// Keys of a chunk of so many units: a sequence has at most 2^30.
+__device__ __forceinline__ int chunk_keys(int units) { return (units < 1 << 23 ? units : 1 << 23) * kUnit; }
+
 // Where key j of a sequence lies: a row of [pages][kv heads][page], negative where there is none.
 struct Pages {
     const int32_t *table;
@@ -131,7 +134,7 @@ struct Work {
         int units;
         const int slot0 = first_chunk(a, slots, number, s, units);
         if (s < 0) return false;
-        const int chunk = units * kUnit;
+        const int chunk = chunk_keys(units);
         of_sequence(a);
         if ((int64_t)(number - slot0) * chunk >= length && number != slot0) return false;
         first = (number - slot0) * chunk;
@@ -196,8 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
     constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32;
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
-    constexpr int PIECES = 32 * T::UNITS / 64, PITCH = 33, STRIDE = 32 * WAVES;
-    constexpr int WAVE_BYTES = most(WIDTH * PITCH * 4, 64 * HD * (int)sizeof(E));
+    constexpr int PIECES = 32 * T::UNITS / 64, STRIDE = 32 * WAVES, WAVE_BYTES = most(32 * HD * 4, 64 * HD * (int)sizeof(E));
     __shared__ __align__(16) char room[WAVES * WAVE_BYTES];
     __shared__ float stat[WAVES][2][32];
     __shared__ uint32_t seen_by[WAVES][32];
@@ -261,12 +263,17 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
         wave_order();
     }
 
-    // ---- the waves' rows: [WIDTH][PITCH] of each in the room of its tiles
+    // ---- the waves' rows, in the room of their tiles: 16-byte units exchanged within a row by its number
+    const int rows = w.mine * group < 32 ? w.mine * group : 32;
     float *mine_o = reinterpret_cast<float *>(room + wave * WAVE_BYTES);
+    if (r < rows) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mine_o[(d * 32 + 8 * (i / 4) + 4 * h + i % 4) * PITCH + r] = o[d][i];
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<v4f *>(mine_o + r * HD + ((d * 8 + 2 * i + h) ^ (r % (HD / 4))) * 4) =
+                    v4f{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    }
     l = both_sum(l);
     if (h == 0) {
         stat[wave][0][r] = m;
@@ -274,7 +281,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
         seen_by[wave][r] = any;
     }
     __syncthreads();
-    for (int i = wave; i < 32 && i < w.mine * group; i += WAVES) {
+    for (int i = wave; i < rows; i += WAVES) {
         float top = kNoKey;
         uint32_t seen = 0;
 #pragma unroll
@@ -294,7 +301,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
             if (d < WIDTH) {
 #pragma unroll
                 for (int v = 0; v < WAVES; ++v)
-                    y[e] = __builtin_fmaf(reinterpret_cast<const float *>(room + v * WAVE_BYTES)[d * PITCH + i], f[v], y[e]);
+                    y[e] = __builtin_fmaf(reinterpret_cast<const float *>(room + v * WAVE_BYTES)[i * HD + ((d / 4) ^ (i % (HD / 4))) * 4 + d % 4], f[v], y[e]);
                 y[e] = seen ? y[e] / sum : 0.0f;
             }
             bad |= !is_finite(y[e]);
@@ -481,7 +488,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
     int of = s;
     const int slot0 = first_chunk(a, slots, -1, of, units);
     const int t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s, tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
-    const int length = length_of(a, s), chunk = units * kUnit, chunks = (length + chunk - 1) / chunk;
+    const int length = length_of(a, s), chunk = chunk_keys(units), chunks = (int)(((int64_t)length + chunk - 1) / chunk);
     if (t < t0 || t - t0 >= tokens || t - t0 >= a.max_rows || chunks <= 1) return;
     const int64_t step = (int64_t)a.kv_heads * most_rows * a.dim;
     const int d0 = lane < a.dim ? lane : 0, d1 = lane + 64 < a.dim ? lane + 64 : 0;

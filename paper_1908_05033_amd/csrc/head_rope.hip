@@ -33,6 +33,7 @@ __device__ __forceinline__ Place place_of(const Share &share, int dim, int pairs
     const int item = threadIdx.x / LANES;
     p.row = item / share.heads;
     p.unit = p.row < share.rows ? blockIdx.y * share.heads + item % share.heads : 1 << 30;
+    if (p.row >= share.rows) p.row = 0;      // (lanes past the last row have nothing to do)
     p.c = threadIdx.x % LANES;
     const int turning = pairs / 8;
     p.turns = p.c < turning;

@@ -28,7 +28,8 @@ def plan(tmp_path_factory):
 
 def test_plan(plan):
     assert plan(1, 32, 8, 1, 512) == dict(tiles=False, single=True, row_tiles=1, slots=0)
-    assert plan(1, 32, 8, 1, 4096) == dict(tiles=False, single=False, row_tiles=1, slots=128)
+    assert plan(1, 32, 8, 1, 4096) == dict(tiles=False, single=False, row_tiles=1, slots=64)
+    assert plan(1, 32, 8, 2, 4096)["slots"] == 128
     assert plan(48, 32, 8, 8, 512) == dict(tiles=True, single=False, row_tiles=2, slots=32)
     assert plan(8, 32, 8, 1, 4096)["tiles"] is False and plan(9, 32, 8, 1, 4096)["tiles"] is True
     assert plan(1 << 20, 1024, 1, 1, 1 << 30)["slots"] == 1

@@ -171,6 +171,20 @@ def test_backward(rows, hq, hk, dim, rope_dim, axes, interleaved, dtype):
             check_grads(x, w, eps, turning, interleaved, g, o, gw, terms, what)
 
 
+@pytest.mark.parametrize("dim,rows", [(8, 100), (16, 9), (32, 33), (256, 5)])
+def test_backward_of_few_heads(dim, rows):
+    """Several rows a workgroup, the last one not full; queries alone, one weight's gradient alone."""
+    q, _, _ = qkv(20, rows, 1, 1, dim, torch.float32)
+    g, w, turning = normal(21, rows, 1, dim), normal(22, dim), rotation(14, rows, dim // 16 * 16)
+    gx, gw = torch.empty(rows, 1, dim, device="cuda"), torch.empty(dim, device="cuda")
+    ws = torch.full((B.dsq_qk_norm_rope_bwd_bytes(rows, 1, 0, dim),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.dsq_qk_norm_rope_bwd(q, None, w, None, EPS, *turning, False, g, None, gx, None, gw, None, ws)
+    check_grads(q, w, EPS, turning, False, g, gx, gw, rows + 256, "q")
+    y = torch.empty_like(gx)
+    B.dsq_qk_norm_rope(q, None, None, w, None, EPS, *turning, False, y, None, None, None, None)
+    check_rope(q, w, EPS, turning, False, y, "q")
+
+
 def test_backward_in_place_and_without_weights():
     q, k, _ = qkv(11, 12, 4, 2, 64, torch.float32)
     g, gk, _ = qkv(12, 12, 4, 2, 64, torch.float32)

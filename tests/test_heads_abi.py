@@ -122,6 +122,8 @@ def test_attention_refusals():
     for page in (0, -16, 24, 1 << 17):
         assert _cache(page=page) == 5
     assert _cache(tp=(1 << 14) + 1, page=1 << 16) == 5 and _cache(rows=1 << 16, n=1 << 16, tp=1 << 12, page=1 << 16) == 5
+    assert _cache(most=1 << 21, hq=1024, hk=1, qr=65536, outr=65536, rows=1, n=1, tp=1) == 5
+    assert _cache(rows=200, n=200, tp=1 << 14, page=1 << 16) == 5
     for name in ("kc", "vc", "table", "lengths", "ws"):
         assert _cache(**{name: None}) == 1, name
         assert _cache(**{name: FAKE + 8}) == 6, name
