@@ -61,7 +61,9 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
-    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, ROWS, tiles - 1 - of);
+    const int number = tile_of_turn(of, tiles, a.sequences);
+    if (number < 0) return;
+    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, ROWS, number);
     if (s.at < 0) return;
 
     const E *kp = (const E *)a.k.p + s.k0 * a.k.row + kv * a.k.head, *vp = (const E *)a.v.p + s.k0 * a.v.row + kv * a.v.head;
@@ -92,14 +94,16 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
     const float c = a.scale * kLog2e;
 
-    Mover<E, HD, KEYS> km, vm;
+    Feed<E, HD, KEYS, sizeof(E) == 2 && BUFFERS == 2> km, vm;
+    const auto start = [&](int t, int b) {
+        E *const to = tiles_at + b * 2 * TILE;
+        km.start(to, kp, a.k.row, t * KEYS, k_end, a.dim);
+        vm.start(to + TILE, vp, a.v.row, t * KEYS, k_end, a.dim);
+    };
     v16f dq[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dq[d] = zeros();
-    if (count > 0) {
-        km.fetch(kp, a.k.row, 0, k_end, a.dim);
-        vm.fetch(vp, a.v.row, 0, k_end, a.dim);
-    }
+    if (count > 0) start(0, 0);
     // One block of keys, in a buffer whose place the compiler knows: p in x, grad_out . v in y, zeros for what is not seen.
     const auto scores = [&](const E *kt, const E *vt, int in, int at, v16f &x, v16f &y) {
         x = y = zeros();
@@ -125,18 +129,17 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     if (sizeof(E) == 2 && k_end <= 128) {
         float sum = 0.0f;
         for (int t = 0; t < count; ++t) {
+            E *const kt = tiles_at + (BUFFERS == 2 ? t & 1 : 0) * 2 * TILE, *const vt = kt + TILE;
+            if (BUFFERS == 1) __syncthreads();
+            km.finish(kt);
+            vm.finish(vt);
             __syncthreads();
-            km.put(tiles_at);
-            vm.put(tiles_at + TILE);
-            __syncthreads();
-            const int next = t + 1 < count ? t + 1 : 0;
-            km.fetch(kp, a.k.row, next * KEYS, k_end, a.dim);
-            vm.fetch(vp, a.v.row, next * KEYS, k_end, a.dim);
+            if (t + 1 < count) start(t + 1, BUFFERS == 2 ? (t + 1) & 1 : 0);
             for (int n = 0; n < KT; ++n) {
                 const int in = (part * KT + n) * 32, at = t * KEYS + in;
                 if (at >= any) break;
                 v16f x, y;
-                scores(tiles_at, tiles_at + TILE, in, at, x, y);
+                scores(kt, vt, in, at, x, y);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(x[i], y[i], sum);
             }
@@ -151,19 +154,18 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
         }
         __syncthreads();
         delta = sum;
+        if (count > 0) start(0, 0);
     }
     if (there && h == 0 && part == 0) a.delta[stat] = delta;
     delta *= kDrop<E>;
     const auto block = [&](int t, auto buffer) {
-        E *const kt = tiles_at + decltype(buffer)::value * 2 * TILE, *const vt = kt + TILE;
+        constexpr int B = decltype(buffer)::value;
+        E *const kt = tiles_at + B * 2 * TILE, *const vt = kt + TILE;
         if (BUFFERS == 1) __syncthreads();
-        km.put(kt);
-        vm.put(vt);
+        km.finish(kt);
+        vm.finish(vt);
         __syncthreads();
-        if (t + 1 < count) {
-            km.fetch(kp, a.k.row, (t + 1) * KEYS, k_end, a.dim);
-            vm.fetch(vp, a.v.row, (t + 1) * KEYS, k_end, a.dim);
-        }
+        if (t + 1 < count) start(t + 1, BUFFERS - 1 - B);
 #pragma unroll
         for (int n = 0; n < KT; ++n) {
             const int in = (part * KT + n) * 32, at = t * KEYS + in;     // the wave's first key, and its place in the tile
@@ -373,7 +375,7 @@ template <class E, int WIDTH, int ROW_WAVES>
 hipError_t queries(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     const int tiles = tiles_of(a, a.q_rows, 32 * ROW_WAVES);
-    attn_bwd_q_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    attn_bwd_q_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)turns_of(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 template <class E, int WIDTH, int KEY_PAIRS, int ROW_PAIRS, int SUB>

@@ -98,6 +98,9 @@ __device__ __forceinline__ void wave_order()
     __builtin_amdgcn_wave_barrier();
 }
 
+// The wave's number within its workgroup, known to the compiler to be the same for all lanes.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // Rows of a tile on their way from memory to LDS: 16 bytes at a time, side by side in a row for lanes side by side.
 template <class E, int HD, int ROWS, int THREADS = 256>
 struct Mover {
@@ -136,15 +139,56 @@ struct Mover {
     }
 };
 
+// Tiles on their way from memory to LDS: start() sends for one, finish() has it there (for this wave; a barrier makes it everyone's).
+// DIRECT: straight into LDS, without registers and stores: 64 lanes of a wave fill 1 KB of a tile side by side, so a lane fetches the
+// unit that belongs in its place.  The tile has to be free from start() on; else from finish() on.
+// (The loads are instructions the compiler does not know of.  They have no registers for it to use early, what it waits for itself
+// it waits for no less long, and finish() waits for all.)
+template <class E, int HD, int ROWS, bool DIRECT>
+struct Feed {
+    typedef Tile<E, HD> T;
+    static constexpr int PIECES = ROWS * T::UNITS / 256, STEP = 256 / T::UNITS;
+    static_assert(!DIRECT || STEP % 16 == 0, "the exchange of units goes by the row's number modulo 16");
+    Mover<E, HD, ROWS> mover;
+    __device__ __forceinline__ void start(E *t, const E *p, int64_t stride, int first, int end, int dim)
+    {
+        if constexpr (!DIRECT) {
+            mover.fetch(p, stride, first, end, dim);
+            return;
+        }
+        const int row = threadIdx.x / T::UNITS, unit = T::place(row, threadIdx.x % T::UNITS) - row * HD, u = unit < dim ? unit : 0;
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)t + wave_number() * 1024;
+        if (first + ROWS <= end && stride <= 1 << 24) {
+            const uint32_t off = ((uint32_t)row * (uint32_t)stride + u) * (uint32_t)sizeof(E);
+            const char *from = reinterpret_cast<const char *>(p + first * stride);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(base + i * 4096), "v"(off),
+                             "s"(from + i * STEP * stride * (int)sizeof(E))
+                             : "memory", "m0");
+        } else {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int j = first + row + STEP * i;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base + i * 4096),
+                             "v"(p + u + (j < end ? j : end - 1) * stride)
+                             : "memory", "m0");
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(E *t)
+    {
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else mover.put(t);
+    }
+};
+
 // Keeps the compiler from computing a rarely taken branch's selections always.
 __device__ __forceinline__ void stay_a_branch() { asm volatile(""); }
 
 // Heads of up to 64, 96 and 128 elements have kernels of their own (WIDTH); rows of a tile have 64 or 128.
 template <int WIDTH>
 constexpr int kRow = WIDTH == 64 ? 64 : 128;
-
-// The wave's number within its workgroup, known to the compiler to be the same for all lanes.
-__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // Schedule of the products just written: FIRST of their READS loads from LDS before the first of MANY products, the others one after each, so
 // that a product does not wait for its own load.
@@ -250,6 +294,14 @@ __device__ __forceinline__ int find_sequence(const int32_t *starts, int rows, in
         if (n <= 1) return __builtin_amdgcn_readfirstlane(lo);
     }
 }
+
+// The tile that is the turn's: the last tiles of a causal prompt are the longest and go first, those of all sequences in turn.
+__device__ __forceinline__ int tile_of_turn(int turn, int tiles, int sequences)
+{
+    const int each = (tiles + sequences - 1) / sequences;
+    return tiles - 1 - turn % sequences * each - turn / sequences;
+}
+inline int turns_of(int tiles, int sequences) { return (tiles + sequences - 1) / sequences * sequences; }
 
 // by_keys: the tiles are of keys.
 __device__ __forceinline__ Sequence tile_of(const int32_t *q_starts, const int32_t *k_starts, int q_rows, int k_rows, int sequences,

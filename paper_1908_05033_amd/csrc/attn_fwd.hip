@@ -18,6 +18,7 @@ struct Fwd {
     static constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 && sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT * SPLIT;
     static constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
     static constexpr int BYTES = most(BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
+    static constexpr bool DIRECT = sizeof(E) == 2 && BUFFERS == 2;
     typedef Tile<E, HD> T;
 };
 
@@ -57,8 +58,9 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
-    // (the last tiles of a causal prompt are the longest: they go first)
-    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, F::ROWS, tiles - 1 - of);
+    const int number = tile_of_turn(of, tiles, a.sequences);
+    if (number < 0) return;
+    const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, F::ROWS, number);
     if (s.at < 0) return;
 
     const E *kp = (const E *)a.k.p + s.k0 * a.k.row + kv * a.k.head, *vp = (const E *)a.v.p + s.k0 * a.v.row + kv * a.v.head;
@@ -77,10 +79,11 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     const int whole = first_row + 31 < s.q_len ? visible(s, a.causal, first_row) : 0;
     const int any = first_row < s.q_len ? visible(s, a.causal, last_row) : 0;
 
-    Mover<E, F::HD, F::KEYS> km, vm;
-    auto fetch = [&](int t) {
-        km.fetch(kp, a.k.row, t * F::KEYS, k_end, a.dim);
-        vm.fetch(vp, a.v.row, t * F::KEYS, k_end, a.dim);
+    Feed<E, F::HD, F::KEYS, F::DIRECT> km, vm;
+    const auto start = [&](int t, int b) {
+        E *const to = reinterpret_cast<E *>(room) + b * 2 * F::TILE;
+        km.start(to, kp, a.k.row, t * F::KEYS, k_end, a.dim);
+        vm.start(to + F::TILE, vp, a.v.row, t * F::KEYS, k_end, a.dim);
     };
     const float c = a.scale * kLog2e;
     float m = kNoKey, l = 0.0f;
@@ -89,12 +92,13 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     for (int d = 0; d < F::DT; ++d) o[d] = zeros();
     // one block of keys, in a buffer whose place the compiler knows
     const auto block = [&](int t, auto buffer) {
-        E *const kt = reinterpret_cast<E *>(room) + decltype(buffer)::value * 2 * F::TILE, *const vt = kt + F::TILE;
+        constexpr int B = decltype(buffer)::value;
+        E *const kt = reinterpret_cast<E *>(room) + B * 2 * F::TILE, *const vt = kt + F::TILE;
         if (F::BUFFERS == 1) __syncthreads();
-        km.put(kt);
-        vm.put(vt);
+        km.finish(kt);
+        vm.finish(vt);
         __syncthreads();
-        if (t + 1 < count) fetch(t + 1);
+        if (t + 1 < count) start(t + 1, F::BUFFERS - 1 - B);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
         if (at < any)
             attend<E, WIDTH, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) {
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
                     for (int i = 0; i < 16; ++i) x[n][i] = n * 32 + 8 * (i / 4) + i % 4 < left ? x[n][i] : -INFINITY;
             });
     };
-    if (count > 0) fetch(0);
+    if (count > 0) start(0, 0);
     for (int t = 0; t < count; t += 2) {
         block(t, std::integral_constant<int, 0>());
         if (t + 1 < count) block(t + 1, std::integral_constant<int, F::BUFFERS - 1>());
@@ -174,7 +178,7 @@ template <class E, int WIDTH, int ROW_WAVES>
 hipError_t launch(const DsqAttnArgs &a, hipStream_t stream)
 {
     const int rows = Fwd<E, WIDTH, ROW_WAVES>::ROWS, tiles = a.q_starts ? a.q_rows / rows + a.sequences : (a.q_rows + rows - 1) / rows;
-    attn_fwd_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)tiles * a.q_heads), 256, 0, stream>>>(a, tiles);
+    attn_fwd_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)turns_of(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 
