@@ -279,7 +279,6 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
             for (int i = 0; i < STEPS; ++i)
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) x[u] = multiply(T::row_operand(rows, part * MINE + u * 32 + r, i, h), own[i], x[u]);
-            if (sizeof(E) == 2) ahead<SUB * STEPS, SUB * STEPS, STEPS>();
             if (VALUES) {
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) {
@@ -322,7 +321,6 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
                     for (int d = 0; d < DT; ++d)
                         sum[d] = multiply(T::column_operand(columns, part * MINE + u * 32 + half * 16, d * 32, lane), w, sum[d]);
                 }
-            if (sizeof(E) == 2) ahead<SUB * 4 * DT, SUB * 2 * DT, 2 * DT>();
         }
     };
     if (values) walk(std::true_type());
