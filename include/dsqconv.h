@@ -510,8 +510,8 @@ dsq_status dsq_linear_w4a8(const int8_t *codes, size_t codes_bytes,
  *   16 bytes, 0 for one that repeats): the parts of one q/k/v tensor are such inputs and such
  *   outputs.  Heads of an output do not overlap (DSQ_ERR_SHAPE).  q_heads is a multiple of
  *   kv_heads; query head i uses key head i / (q_heads / kv_heads).  dim is a multiple of 8, at
- *   most 128 (256 for norm and rotation), and there are at most 1024 heads and 2^16 sequences:
- *   DSQ_ERR_UNSUPPORTED beyond.
+ *   most 128 (256 for norm and rotation), and there are at most 2^21 rows, 1024 heads and 2^16
+ *   sequences: DSQ_ERR_UNSUPPORTED beyond.
  *   Packed sequences lie one behind the other: sequence s has the rows starts[s] ..
  *   starts[s + 1] - 1 (int32 [sequences + 1], not falling); rows of outputs before the first and
  *   behind the last sequence are left as they were.  Starts outside the rows are taken
@@ -595,7 +595,8 @@ dsq_status dsq_qk_norm_rope_bwd(const void *q, int64_t q_row, int64_t q_head,
  * does not see has no part in it, infinities and NaN included.
  *
  * q_starts, k_starts   device; k_starts NULL: as q_starts; both NULL: one sequence of all rows
- *            (sequences = 1)
+ *            (sequences = 1); heads times (rows / 64 + 2 sequences) are at most 3 * 2^21, of queries
+ *            and of keys (DSQ_ERR_UNSUPPORTED)
  * scale      finite and > 0 (DSQ_ERR_RANGE); scores scale * q . k stay inside binary32
  * lse        device, out, float32 [q_heads][q_rows]: log of the sum of exp(scale * q . k), -inf for
  *            a row that sees no key, for the backward pass; or NULL
@@ -613,7 +614,7 @@ dsq_status dsq_attention(const void *q, int64_t q_row, int64_t q_head, const voi
  * Gradients of a key head are the sums over the query heads that share it.  No atomics: the same
  * result every time.  An infinity or NaN spoils the gradients of its own sequence and of no other.
  * In float16 products ds = p * (grad_out . v - out . grad_out) below 2^-14 lose digits and below
- * 2^-25 vanish: such programs scale their loss.
+ * 2^-25 vanish, and above 65504 are infinite: such programs scale their loss.
  *
  * grad_q, grad_k, grad_v   device, out; overlap no input
  * workspace  device, dsq_attention_bwd_bytes(q_rows, q_heads) bytes; of no other call that may
@@ -653,7 +654,9 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
  * workspace  device, dsq_attention_cache_bytes(..) bytes; of no other call that may run at the same
  *            time, captured graphs included
  * A sequence has at most 2^30 keys (table_pages * page), all sequences together 2^37 by their tables, and
- * max_rows times the heads that share a key head are at most 2^30 (DSQ_ERR_UNSUPPORTED).
+ * max_rows times the heads that share a key head are at most 2^30; rows times q_heads are below 2^26, and
+ * sequences times kv_heads, times 128s of rows a key head where there are more than 32, below 2^22
+ * (DSQ_ERR_UNSUPPORTED).
  */
 dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head,
                                dsq_dtype dtype, int rows, int q_heads, int kv_heads,

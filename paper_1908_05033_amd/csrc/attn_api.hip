@@ -173,6 +173,9 @@ dsq_status dsq_qk_norm_rope_bwd(const void *q, int64_t q_row, int64_t q_head, co
 
 namespace {
 
+// A launch has fewer than 2^32 threads: tiles of 64 rows or more, and at most two more a sequence, of up to 512 threads.
+bool tiles_fit(int rows, int heads, int sequences) { return (rows / 64 + 2LL * sequences) * heads <= 3 << 21; }
+
 // What the calls of attention have in common.
 dsq_status attention_ok(dsq_dtype dtype, int q_rows, int q_heads, int kv_heads, int dim, int sequences, float scale)
 {
@@ -182,10 +185,10 @@ dsq_status attention_ok(dsq_dtype dtype, int q_rows, int q_heads, int kv_heads, 
     if (!(scale > 0.0f && isfinite(scale))) return DSQ_ERR_RANGE;
     return DSQ_OK;
 }
-dsq_status prompts_ok(int q_rows, int k_rows, int sequences, const int32_t *q_starts, const int32_t *k_starts)
+dsq_status prompts_ok(int q_rows, int k_rows, int q_heads, int kv_heads, int sequences, const int32_t *q_starts, const int32_t *k_starts)
 {
     if (k_rows < 0 || (!q_starts && sequences != 1)) return DSQ_ERR_SHAPE;
-    if (k_rows > kMaxRows) return DSQ_ERR_UNSUPPORTED;
+    if (k_rows > kMaxRows || !tiles_fit(q_rows, q_heads, sequences) || !tiles_fit(k_rows, kv_heads, sequences)) return DSQ_ERR_UNSUPPORTED;
     if (!q_starts && k_starts) return DSQ_ERR_NULL;
     if (!aligned16(q_starts) || !aligned16(k_starts)) return DSQ_ERR_ALIGN;
     return DSQ_OK;
@@ -201,7 +204,7 @@ dsq_status dsq_attention(const void *q, int64_t q_row, int64_t q_head, const voi
                          int64_t out_row, int64_t out_head, float *lse, void *hip_stream)
 {
     TRY(attention_ok(dtype, q_rows, q_heads, kv_heads, dim, sequences, scale));
-    TRY(prompts_ok(q_rows, k_rows, sequences, q_starts, k_starts));
+    TRY(prompts_ok(q_rows, k_rows, q_heads, kv_heads, sequences, q_starts, k_starts));
     if (q_rows == 0 || sequences == 0) return DSQ_OK;
     if (!q || !out || (k_rows && (!k || !v))) return DSQ_ERR_NULL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(lse)) return DSQ_ERR_ALIGN;
@@ -226,7 +229,7 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
                              size_t workspace_bytes, void *hip_stream)
 {
     TRY(attention_ok(dtype, q_rows, q_heads, kv_heads, dim, sequences, scale));
-    TRY(prompts_ok(q_rows, k_rows, sequences, q_starts, k_starts));
+    TRY(prompts_ok(q_rows, k_rows, q_heads, kv_heads, sequences, q_starts, k_starts));
     if ((q_rows == 0 && k_rows == 0) || sequences == 0) return DSQ_OK;
     if ((q_rows && (!q || !out || !lse || !grad_out || !grad_q || !workspace)) || (k_rows && (!k || !v || !grad_k || !grad_v))) return DSQ_ERR_NULL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(lse) || !aligned16(grad_out) || !aligned16(grad_q) ||
@@ -266,7 +269,8 @@ dsq_status dsq_attention_cache(const void *q, int64_t q_row, int64_t q_head, dsq
     if (max_rows > kMaxRows || pages > 0x7fffffff || bits < 0 || (int64_t)table_pages << bits > kMaxKeys) return DSQ_ERR_UNSUPPORTED;
     if (rows == 0 || sequences == 0) return DSQ_OK;
     const AttnCachePlan p = attn_cache_plan(max_rows, q_heads, kv_heads, sequences, (int64_t)table_pages << bits);
-    if ((int64_t)(p.slots + sequences) * p.row_tiles * kv_heads > 0x7fffffff || (int64_t)rows * q_heads > 0x7fffffff ||
+    // (a launch has fewer than 2^32 threads: 512 a chunk, 64 a row and head or four)
+    if ((int64_t)sequences * p.row_tiles * kv_heads >= 1 << 22 || (int64_t)rows * q_heads >= 1 << 26 ||
         (((int64_t)table_pages << bits) / 128 + 1) * sequences > 1 << 30 || (int64_t)max_rows * (q_heads / kv_heads) > 1 << 30)
         return DSQ_ERR_UNSUPPORTED;
     if (!q || !out || !lengths || !workspace || (pages && (!k_cache || !v_cache)) || (table_pages && !page_table)) return DSQ_ERR_NULL;

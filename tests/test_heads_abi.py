@@ -131,6 +131,19 @@ def test_attention_refusals():
     assert _cache(rows=0, qs=FAKE, q=None) == 0
 
 
+def test_refuses_launches_of_too_many_threads():
+    """A launch has fewer than 2^32 threads.  (Without pointers: what is not refused for its size is for them, and nothing is launched.)"""
+    apart = dict(qr=1024 * 64, outr=1024 * 64, hq=1024, hk=1024, kr=1024 * 64, vr=1024 * 64, q=None)
+    for f in (_attn, _attn_bwd):
+        for rows, keys, n, want in ((1 << 21, 4, 1, 5), (4, 1 << 21, 1, 5), (392960, 4, 1, 1), (4, 392960, 1, 1), (393216, 4, 1, 5), (4, 393216, 1, 5),
+                                    (4, 4, 3000, 1), (4, 4, 3200, 5), (4, 4, 1 << 16, 5)):
+            assert f(**apart, rows=rows, keys=keys, n=n, qs=FAKE) == want, (rows, keys, n)
+    apart = dict(qr=1024 * 64, outr=1024 * 64, hq=1024, q=None)
+    for rows, n, hk, want in ((1 << 16, 1 << 16, 8, 5), ((1 << 16) - 1, (1 << 16) - 1, 32, 1), (1 << 15, 1 << 15, 128, 5), ((1 << 15) - 1, (1 << 15) - 1, 128, 1)):
+        assert _cache(**apart, rows=rows, n=n, hk=hk) == want, (rows, n, hk)
+    assert _cache(**apart, rows=4, n=4, hk=8, most=1 << 21) == 5 and _cache(**apart, rows=4, n=1, hk=8, most=1 << 17, qs=FAKE) == 1
+
+
 def test_binding_takes_device_tensors_alone():
     x, u8, i32 = torch.zeros(4, 2, 64), torch.zeros(1 << 16, dtype=torch.uint8), torch.zeros(5, dtype=torch.int32)
     c = torch.zeros(2, 2, 16, 64)
