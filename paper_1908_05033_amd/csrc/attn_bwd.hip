@@ -7,6 +7,10 @@
 // time.  One owns rows of queries (D and dq), the other keys, over all heads that share them (dk and dv).  In both a
 // lane holds a column of the 32x32 results, so probabilities and ds are the second operand of the next product as they lie
 // in registers (attn_device.h).
+//
+// Seven products of the scores' size, where one kernel with atomics would have five.  Measured, bfloat16, 4 x 2048 rows, causal, 16 heads
+// of 128 in four groups: queries 120 us (45 % of the matrix units' cycles), keys 200 us (34 %; LDS 37 %: one workgroup of eight waves a
+// compute unit goes through its phases in step).  binary32, 80 elements, 3 sequences of up to 701 rows: 48 and 55 us, few workgroups of one wave a SIMD.
 #include <type_traits>
 
 #include "attn_device.h"

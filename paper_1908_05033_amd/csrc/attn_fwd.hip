@@ -6,6 +6,11 @@
 // wave 32 of them; tiles of keys and values go through LDS, the next tile's loads under way.  Scores are formed transposed, K Q^T,
 // so that a lane holds one row's scores: maximum, sum and the factor of a raised maximum need no exchange but one between the two
 // lanes of a row, and the probabilities are the second operand of V^T P^T as they lie in registers (attn_device.h).
+//
+// Bound by the matrix units and the vector instructions of the softmax beside them: two waves a SIMD, one's products under the other's
+// exponentials.  Measured, bfloat16, 128 elements, causal: 16384 rows, 16 heads 1114 us (987 TFLOP/s; a library product of 8192^3 reaches
+// 1131; 52 % of the matrix units' cycles), 4096 rows, 32 heads 149 us (925).  float16, 64 elements, 16 sequences of up to 1000
+// rows 34 us: the walk over the longest one's keys.
 #include <type_traits>
 
 #include "attn_device.h"

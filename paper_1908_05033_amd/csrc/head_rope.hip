@@ -7,7 +7,9 @@
 // A lane holds both elements of eight pairs, 16 of a head's elements in two units of eight: pairs of halves are the units c and
 // rope_dim / 16 + c, neighbouring pairs, and the elements behind the rotated ones, the units 2c and 2c + 1.  Angles are
 // formed once a row and workgroup, the product and its remainder in binary64: a position of 2^31 still has its angle to 2^-20.
-// Bound by HBM bandwidth, and by latency for a few rows.
+// Bound by HBM bandwidth, and by latency for a few rows.  Measured: bfloat16, 4096 rows, 32 + 8 heads of 128 and a cache, 101 MB,
+// 25.5 us (4.0 TB/s; a row's 256 bytes of a cached head go to a place of their own: 21.3 with neighbouring slots); 8 rows 4.2 us;
+// binary32, 80 elements, both passes 128 MB, 45 us (five of eight lanes are busy).
 #include "attn_device.h"
 
 namespace {
