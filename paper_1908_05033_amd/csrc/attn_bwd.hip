@@ -213,11 +213,11 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
     typedef Tile<E, HD> T;
     typedef typename Operand<E>::type V8;
     constexpr int PAIRS = KEY_PAIRS * ROW_PAIRS, THREADS = 128 * PAIRS, KEYS = 32 * KEY_PAIRS, MINE = 32 * SUB, ROWS = MINE * ROW_PAIRS;
-    constexpr int TILE = ROWS * HD, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
-    __shared__ __align__(16) char room[most(2 * TILE * (int)sizeof(E), JOIN)];
+    // Tiles of queries (and of gradients, where 160 KB have room) go straight into a second buffer: 1 to 4 % of both backward kernels' time.
+    constexpr bool DIRECT_Q = sizeof(E) == 2, DIRECT_G = sizeof(E) == 2 && WIDTH == 64;
+    constexpr int TILE = ROWS * HD, TILES = 2 + DIRECT_Q + DIRECT_G, JOIN = (ROW_PAIRS - 1) * 2 * KEY_PAIRS * DT * 4096;
+    __shared__ __align__(16) char room[most(TILES * TILE * (int)sizeof(E), JOIN)];
     __shared__ __align__(16) float handed[PAIRS][SUB][16 * 64], stats[2][ROWS];
-
-    E *const qt = reinterpret_cast<E *>(room), *const gt = qt + TILE;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), r = lane & 31, h = lane >> 5;
     const int pair = wave % PAIRS, part = pair / KEY_PAIRS, group = a.q_heads / a.kv_heads;
@@ -243,11 +243,14 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
     const int all = a.causal ? first_key - off + 31 : 0;
     const float c = a.scale * kLog2e;
 
-    Mover<E, HD, ROWS, THREADS> qm, gm;
+    Feed<E, HD, ROWS, DIRECT_Q, THREADS> qm;
+    Feed<E, HD, ROWS, DIRECT_G, THREADS> gm;
+    const auto q_tile = [&](int b) { return reinterpret_cast<E *>(room) + (DIRECT_Q ? b * TILE : 0); };
+    const auto g_tile = [&](int b) { return reinterpret_cast<E *>(room) + (1 + DIRECT_Q + (DIRECT_G ? b : 0)) * TILE; };
     float stat = 0.0f;
-    auto fetch = [&](int head, int at) {
-        qm.fetch((const E *)a.q.p + s.q0 * a.q.row + head * a.q.head, a.q.row, at, s.q_len, a.dim);
-        gm.fetch((const E *)a.grad_out.p + s.q0 * a.grad_out.row + head * a.grad_out.head, a.grad_out.row, at, s.q_len, a.dim);
+    auto fetch = [&](int head, int at, int b) {
+        qm.start(q_tile(b), (const E *)a.q.p + s.q0 * a.q.row + head * a.q.head, a.q.row, at, s.q_len, a.dim);
+        gm.start(g_tile(b), (const E *)a.grad_out.p + s.q0 * a.grad_out.row + head * a.grad_out.head, a.grad_out.row, at, s.q_len, a.dim);
         if (tid < 2 * ROWS) {
             const int row = at + tid % ROWS;
             const float *numbers = (tid < ROWS ? a.lse : a.delta) + (int64_t)head * a.q_rows + s.q0;
@@ -263,18 +266,19 @@ __global__ __launch_bounds__(128 * KEY_PAIRS * ROW_PAIRS, KEY_PAIRS * ROW_PAIRS 
         constexpr bool VALUES = decltype(role)::value;
         int left = (int)((int64_t)blocks * group * (split + 1) / splits) - from;
         int head = blocks ? kv * group + from / blocks : 0, at = blocks ? first + from % blocks * ROWS : 0;
-        if (left > 0) fetch(head, at);
+        if (left > 0) fetch(head, at, 0);
         v4f *const slot = reinterpret_cast<v4f *>(handed[pair][0]) + lane;
-        for (; left > 0; --left) {
+        for (int b = 0; left > 0; --left, b ^= 1) {
+            E *const qt = q_tile(b), *const gt = g_tile(b);
             __syncthreads();
-            qm.put(qt);
-            gm.put(gt);
+            qm.finish(qt);
+            gm.finish(gt);
             if (tid < 2 * ROWS) stats[tid / ROWS][tid % ROWS] = tid < ROWS ? __builtin_fmaf(stat, kLog2e, -kLift<E>) : stat * kDrop<E>;
             __syncthreads();
             const int row0 = at + part * MINE;                      // the wave's first row
             at += ROWS;
             if (at >= s.q_len) at = first, ++head;
-            if (left > 1) fetch(head, at);
+            if (left > 1) fetch(head, at, b ^ 1);
             v16f x[SUB];
             const E *rows = VALUES ? qt : gt;
 #pragma unroll

@@ -144,12 +144,12 @@ struct Mover {
 // unit that belongs in its place.  The tile has to be free from start() on; else from finish() on.
 // (The loads are instructions the compiler does not know of.  They have no registers for it to use early, what it waits for itself
 // it waits for no less long, and finish() waits for all.)
-template <class E, int HD, int ROWS, bool DIRECT>
+template <class E, int HD, int ROWS, bool DIRECT, int THREADS = 256>
 struct Feed {
     typedef Tile<E, HD> T;
-    static constexpr int PIECES = ROWS * T::UNITS / 256, STEP = 256 / T::UNITS;
+    static constexpr int PIECES = ROWS * T::UNITS / THREADS, STEP = THREADS / T::UNITS;
     static_assert(!DIRECT || STEP % 16 == 0, "the exchange of units goes by the row's number modulo 16");
-    Mover<E, HD, ROWS> mover;
+    Mover<E, HD, ROWS, THREADS> mover;
     __device__ __forceinline__ void start(E *t, const E *p, int64_t stride, int first, int end, int dim)
     {
         if constexpr (!DIRECT) {
@@ -163,14 +163,14 @@ struct Feed {
             const char *from = reinterpret_cast<const char *>(p + first * stride);
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(base + i * 4096), "v"(off),
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(base + i * THREADS * 16), "v"(off),
                              "s"(from + i * STEP * stride * (int)sizeof(E))
                              : "memory", "m0");
         } else {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int j = first + row + STEP * i;
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base + i * 4096),
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base + i * THREADS * 16),
                              "v"(p + u + (j < end ? j : end - 1) * stride)
                              : "memory", "m0");
             }
