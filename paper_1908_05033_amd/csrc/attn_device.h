@@ -269,6 +269,43 @@ __device__ __forceinline__ typename Operand<E>::type load_unit8(const E *row, in
     return v;
 }
 
+// Operands of 32 keys straight from memory, for a wave that shares its keys with no other.  binary32 alone: a column's elements are whole
+// words of a lane.  Keys from `end` on are the last one again, elements past a head's its first (as a Mover's).
+template <int WIDTH>
+struct RowOperands {
+    v8f at[WIDTH / 16];
+    __device__ __forceinline__ void fetch(const float *p, int64_t stride, int first, int end, int dim, int lane)
+    {
+        const int j = first + (lane & 31), h = lane >> 5;
+        const float *row = p + (j < end ? j : end - 1) * stride;
+#pragma unroll
+        for (int i = 0; i < WIDTH / 16; ++i) {
+            const float *from = row + ((2 * i + h) * 8 < dim ? (2 * i + h) * 8 : 0);
+            at[i] = __builtin_shufflevector(*reinterpret_cast<const v4f *>(from), *reinterpret_cast<const v4f *>(from + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+};
+template <int WIDTH>
+struct ColumnOperands {
+    v8f at[2][WIDTH / 32];
+    __device__ __forceinline__ void fetch(const float *p, int64_t stride, int first, int end, int dim, int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+        const bool whole = first + 32 <= end && stride <= 1 << 24;
+        const char *from = reinterpret_cast<const char *>(p + first * stride);
+#pragma unroll
+        for (int d = 0; d < WIDTH / 32; ++d) {
+            const int u = d * 32 + r < dim ? d * 32 + r : 0;
+            const uint32_t off = ((uint32_t)(4 * h) * (uint32_t)stride + u) * 4;
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+                const int key = n / 8 * 16 + n / 4 % 2 * 8 + n % 4, j = first + 4 * h + key;
+                at[n / 8][d][n % 8] = whole ? *reinterpret_cast<const float *>(from + key * stride * 4 + off) : p[(j < end ? j : end - 1) * stride + u];
+            }
+        }
+    }
+};
+
 // ---- packed sequences ---------------------------------------------------------------------------
 //
 // Tiles of `tile` rows: sequence s has its own from number starts[s] / tile + s on, which leaves room for as many as it
@@ -340,20 +377,18 @@ constexpr float kNoKey = -3.0e38f;
 
 // ---- a block of keys ----------------------------------------------------------------------------------
 //
-// 32 KT keys, from row `in` of the tiles kt and vt on, for the 32 rows of a wave: running maximum m and sum l (of the scores times c, to
-// base 2) of the lane's row and the transposed sums o.  `hide` puts -inf in the place of scores that are not seen.
-template <class E, int WIDTH, int KT, class Hide>
-__device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[WIDTH / 16], float c, float &m, float &l,
-                                       v16f (&o)[WIDTH / 32], int lane, Hide hide)
+// 32 KT keys for the 32 rows of a wave: running maximum m and sum l (of the scores times c, to base 2) of the lane's row and the
+// transposed sums o.  key(n, i) and value(n, half, d) are the operands of 32 keys n, `hide` puts -inf in the place of scores that are not seen.
+template <class E, int WIDTH, int KT, class Key, class Value, class Hide>
+__device__ __forceinline__ void attend_to(Key key, Value value, const typename Operand<E>::type (&q)[WIDTH / 16], float c, float &m, float &l,
+                                          v16f (&o)[WIDTH / 32], Hide hide)
 {
-    typedef Tile<E, kRow<WIDTH>> T;
-    const int r = lane & 31, h = lane >> 5;
     v16f x[KT];
 #pragma unroll
     for (int n = 0; n < KT; ++n) {
         x[n] = zeros();
 #pragma unroll
-        for (int i = 0; i < WIDTH / 16; ++i) x[n] = multiply(T::row_operand(kt, in + n * 32 + r, i, h), q[i], x[n]);
+        for (int i = 0; i < WIDTH / 16; ++i) x[n] = multiply(key(n, i), q[i], x[n]);
     }
     if (sizeof(E) == 2) ahead<KT * WIDTH / 16, KT * WIDTH / 16, 6>();        // (2 % of a long prompt's time)
     hide(x);
@@ -386,8 +421,17 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
         for (int half = 0; half < 2; ++half) {
             const typename Operand<E>::type p = operand_of<E>(x[n], half);
 #pragma unroll
-            for (int d = 0; d < WIDTH / 32; ++d) o[d] = multiply(T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane), p, o[d]);
+            for (int d = 0; d < WIDTH / 32; ++d) o[d] = multiply(value(n, half, d), p, o[d]);
         }
+}
+// The same from row `in` of the tiles kt and vt on.
+template <class E, int WIDTH, int KT, class Hide>
+__device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const typename Operand<E>::type (&q)[WIDTH / 16], float c, float &m, float &l,
+                                       v16f (&o)[WIDTH / 32], int lane, Hide hide)
+{
+    typedef Tile<E, kRow<WIDTH>> T;
+    attend_to<E, WIDTH, KT>([&](int n, int i) { return T::row_operand(kt, in + n * 32 + (lane & 31), i, lane >> 5); },
+                            [&](int n, int half, int d) { return T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane); }, q, c, m, l, o, hide);
 }
 
 // ---- a row formed again ---------------------------------------------------------------------------

@@ -22,7 +22,10 @@ template <class E, int WIDTH, int ROW_WAVES>
 struct Fwd {
     static constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 && sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT * SPLIT;
     static constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
-    static constexpr int BYTES = most(BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
+    // binary32 keys that one wave reads alone need no LDS and no barriers: 6 % less time at 128 elements, 15 % at 96, but at 64 (where two
+    // workgroups share a compute unit) 5 to 40 % more.
+    static constexpr bool NEAR = sizeof(E) == 4 && ROW_WAVES == 1 && WIDTH > 64;
+    static constexpr int BYTES = most(NEAR ? 0 : BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
     static constexpr bool DIRECT = sizeof(E) == 2 && BUFFERS == 2;
     typedef Tile<E, HD> T;
 };
@@ -33,7 +36,7 @@ struct Fwd {
 //                   1024 x 8   2048 x 8   1024 x 32   2048 x 16   4096 x 8
 //   bfloat16, 128   26 / 20    46 / 40    28 / 54     48 / 78     88 / 127
 //   bfloat16, 64    18 / 12    31 / 20    19 / 21     32 / 31     58 / 49
-//   binary32, 128   144 / 58   283 / 123  146 / 146   284 / 246   559 / 444
+//   binary32, 128   144 / 55   283 / 114  146 / 139   284 / 228   559 / 405
 template <class E, int WIDTH>
 constexpr int64_t kFew = sizeof(E) == 2 && WIDTH > 64 ? 32768 : 49152;
 
@@ -95,6 +98,16 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     v16f o[F::DT];
 #pragma unroll
     for (int d = 0; d < F::DT; ++d) o[d] = zeros();
+    const auto hide = [&](auto &x, int at) {
+        constexpr int KT = sizeof(x) / sizeof(v16f);
+        if (at + 32 * KT <= whole) return;
+        stay_a_branch();
+        const int left = seen - at - 4 * h;
+#pragma unroll
+        for (int n = 0; n < KT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = n * 32 + 8 * (i / 4) + i % 4 < left ? x[n][i] : -INFINITY;
+    };
     // one block of keys, in a buffer whose place the compiler knows
     const auto block = [&](int t, auto buffer) {
         constexpr int B = decltype(buffer)::value;
@@ -106,20 +119,31 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
         if (t + 1 < count) start(t + 1, F::BUFFERS - 1 - B);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
         if (at < any)
-            attend<E, WIDTH, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) {
-                if (at + 32 * F::KT <= whole) return;
-                stay_a_branch();
-                const int left = seen - at - 4 * h;
-#pragma unroll
-                for (int n = 0; n < F::KT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[n][i] = n * 32 + 8 * (i / 4) + i % 4 < left ? x[n][i] : -INFINITY;
-            });
+            attend<E, WIDTH, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) { hide(x, at); });
     };
-    if (count > 0) start(0, 0);
-    for (int t = 0; t < count; t += 2) {
-        block(t, std::integral_constant<int, 0>());
-        if (t + 1 < count) block(t + 1, std::integral_constant<int, F::BUFFERS - 1>());
+    if constexpr (F::NEAR) {
+        // each operand of the next block is sent for when this block's has been used
+        RowOperands<WIDTH> ks;
+        ColumnOperands<WIDTH> vs;
+        if (part * 32 < any) {
+            ks.fetch(kp, a.k.row, part * 32, k_end, a.dim, lane);
+            vs.fetch(vp, a.v.row, part * 32, k_end, a.dim, lane);
+        }
+        for (int at = part * 32; at < any; at += F::KEYS) {
+            const int next = at + F::KEYS < any ? at + F::KEYS : at;
+            attend_to<E, WIDTH, 1>([&](int, int i) { return ks.at[i]; }, [&](int, int half, int d) { return vs.at[half][d]; }, q, c, m, l, o,
+                                   [&](v16f (&x)[1]) {
+                                       ks.fetch(kp, a.k.row, next, k_end, a.dim, lane);
+                                       hide(x, at);
+                                   });
+            vs.fetch(vp, a.v.row, next, k_end, a.dim, lane);
+        }
+    } else {
+        if (count > 0) start(0, 0);
+        for (int t = 0; t < count; t += 2) {
+            block(t, std::integral_constant<int, 0>());
+            if (t + 1 < count) block(t + 1, std::integral_constant<int, F::BUFFERS - 1>());
+        }
     }
 
     l = both_sum(l);
