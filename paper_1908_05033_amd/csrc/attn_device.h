@@ -430,8 +430,9 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
                                        v16f (&o)[WIDTH / 32], int lane, Hide hide)
 {
     typedef Tile<E, kRow<WIDTH>> T;
-    attend_to<E, WIDTH, KT>([&](int n, int i) { return T::row_operand(kt, in + n * 32 + (lane & 31), i, lane >> 5); },
-                            [&](int n, int half, int d) { return T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane); }, q, c, m, l, o, hide);
+    const int r = lane & 31, h = lane >> 5;
+    attend_to<E, WIDTH, KT>([=](int n, int i) { return T::row_operand(kt, in + n * 32 + r, i, h); },
+                            [=](int n, int half, int d) { return T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane); }, q, c, m, l, o, hide);
 }
 
 // ---- a row formed again ---------------------------------------------------------------------------
