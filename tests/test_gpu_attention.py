@@ -167,6 +167,33 @@ def test_what_is_not_seen_has_no_part(dtype):
             assert torch.isnan(c.out[40:70, :2]).all()
 
 
+@pytest.mark.parametrize("dim", [72, 80, 96, 104, 128])
+def test_binary32_keys_without_lds(dim):
+    """Wide heads of few rows read keys and values straight from memory: odd lengths, blocks that end inside 32 keys, strides, a long row,
+    and infinities and NaN behind what is seen."""
+    for n, m, causal in ((1, 1, True), (3, 31, True), (33, 33, True), (63, 65, False), (31, 129, True), (129, 127, True), (100, 225, False)):
+        c = call(n + m, "f32", [n], [m], 4, 2, dim, causal)
+        c.forward().backward().check()
+    c = call(1, "f32", [5, 0, 61, 1], [40, 3, 90, 1], 4, 2, dim, first=3, behind=2)
+    c.forward().backward().check()
+    # rows 2^24 elements and more apart: addresses of their own for each lane
+    apart = torch.empty_strided((40, 2, dim), ((1 << 24) + 4, 128, 1), dtype=torch.float32, device="cuda")
+    k = normal(2, 40, 2, dim, dtype=torch.float32)
+    apart.copy_(k)
+    q = normal(3, 40, 4, dim, dtype=torch.float32)
+    a, b = Call(q, k, k, None, None).forward(), Call(q, apart, apart, None, None).forward()
+    a.check()
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+    for bad in (NAN, INF):
+        c = call(4, "f32", [70], [70], 2, 1, dim, grad=False)
+        clean = Call(c.q, c.k, c.v, None, None).forward()
+        c.k, c.v = c.k.contiguous(), c.v.contiguous()
+        c.k[50:], c.v[50:] = bad, bad
+        c.forward()
+        check_prompt(c.q, c.k[:50], c.v[:50], [0, 50], [0, 50], True, c.scale, c.out[:50], c.lse[:, :50])
+        assert torch.equal(c.out[:32], clean.out[:32]) and not torch.isfinite(c.out[50:]).any()
+
+
 def test_values_near_the_end_of_their_type():
     """Sums that pass the type's range on the way, not in the result."""
     for dt, big in ((torch.bfloat16, 3e38), (torch.float32, 3e38), (torch.float16, 6e4)):
