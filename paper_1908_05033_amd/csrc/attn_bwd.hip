@@ -368,9 +368,9 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(DsqAttnBwdArgs a, in
 // rows a workgroup:
 //
 //                   1024 x 8    2048 x 8    1024 x 32   2048 x 16   4096 x 8
-//   bfloat16, 128   76 / 59     119 / 92    91 / 111    131 / 147   232 / 238
-//   bfloat16, 64    54 / 41     85 / 59     62 / 59     91 / 77     162 / 124
-//   binary32, 128   190 / 142   402 / 330   335 / 380   603 / 653   1136 / 1200
+//   bfloat16, 128   63 / 57     97 / 93     76 / 111    107 / 147   186 / 236
+//   bfloat16, 64    45 / 39     68 / 57     54 / 58     74 / 75     129 / 121
+//   binary32, 128   183 / 145   397 / 338   335 / 391   599 / 669   1131 / 1225
 template <class E, int WIDTH>
 constexpr int64_t kFew = sizeof(E) == 2 && WIDTH == 64 ? 49152 : 32768;
 

@@ -34,9 +34,9 @@ struct Fwd {
 // keys.  Us, 128 rows / 32 rows a workgroup, rows x heads (causal):
 //
 //                   1024 x 8   2048 x 8   1024 x 32   2048 x 16   4096 x 8
-//   bfloat16, 128   26 / 20    46 / 40    28 / 54     48 / 78     88 / 127
-//   bfloat16, 64    18 / 12    31 / 20    19 / 21     32 / 31     58 / 49
-//   binary32, 128   144 / 55   283 / 114  146 / 139   284 / 228   559 / 405
+//   bfloat16, 128   22 / 16    41 / 33    24 / 45     42 / 65     77 / 103
+//   bfloat16, 64    19 / 11    34 / 19    19 / 19     34 / 25     62 / 40
+//   binary32, 128   144 / 55   284 / 114  146 / 140   284 / 228   559 / 406
 template <class E, int WIDTH>
 constexpr int64_t kFew = sizeof(E) == 2 && WIDTH > 64 ? 32768 : 49152;
 
