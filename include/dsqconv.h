@@ -520,7 +520,8 @@ dsq_status dsq_linear_w4a8(const int8_t *codes, size_t codes_bytes,
  *   of two up to 2^16.
  *   Outputs overlap neither inputs nor each other where a call does not say so.
  *   Sums, softmax and products are binary32; probabilities (and in the backward pass ds) are rounded
- *   to dtype where they meet values in the matrix instruction.
+ *   to dtype where they meet values in the matrix instruction (in float16 times a power of two: a
+ *   probability keeps all digits down to 2^-27 of its row's largest, and counts down to 2^-38).
  */
 size_t dsq_qk_norm_rope_bwd_bytes(int rows, int q_heads, int kv_heads, int dim);
 size_t dsq_attention_bwd_bytes(int q_rows, int q_heads);

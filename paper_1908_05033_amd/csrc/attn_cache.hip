@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
             }
             bad |= !is_finite(y[e]);
         }
-        float log2 = top + __builtin_amdgcn_logf(sum);
+        float log2 = top + __builtin_amdgcn_logf(sum * kSumDrop<E>);
         if (__any(bad)) log2 = again<E>(a, w, pages, kv, i, c, y);
         leave_row<E>(a, w, slots, number, kv, i, seen != 0, log2, y);
     }
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
     // The rows lie transposed in registers: through LDS, a wave's in the room of its tile (units exchanged as in a tile).
     float *mine_o = reinterpret_cast<float *>(&tiles_at[0][0][0]) + wave * TILE * (int)sizeof(E) / 4;
     l = both_sum(l);
-    const float inv = any ? 1.0f / l : 0.0f, log2 = m + __builtin_amdgcn_logf(l);
+    const float inv = any ? 1.0f / l : 0.0f, log2 = m + __builtin_amdgcn_logf(l * kSumDrop<E>);
     bool bad = false;
 #pragma unroll
     for (int d = 0; d < DT; ++d)

@@ -5,6 +5,8 @@
 // i = 8s .. 8s + 7 of a result are therefore an operand of step s of the next product without any exchange between lanes, whose
 // other operand takes its k in the same order: rows 16 s + 4 h + 0 .. 3 and 16 s + 8 + 4 h + 0 .. 3 of a tile ("columns" below).
 #pragma once
+#include <type_traits>
+
 #include "attn_kernels.h"
 #include "lm_device.h"
 
@@ -374,11 +376,23 @@ __device__ __forceinline__ int visible(const Sequence &s, int causal, int i)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A softmax's reference before its first key: below every score, and finite, so that differences with it are numbers.
 constexpr float kNoKey = -3.0e38f;
+// The reference may lag behind the largest score by kLag (to base 2): up to there sums and operands lose nothing, and raising it takes 64
+// products a lane.  In float16, where an operand below 2^-14 loses digits and one of 2^-25 is zero, probabilities enter sums and products times
+// 2^kSumLift, of which results are free, and the reference lags less, so that they stay below 2^15: a probability has all its digits from 2^-27 of
+// its row's largest on, and 2^21 keys that vanish are at most 2^-17 of a row.
+template <class E>
+constexpr bool kLifted = std::is_same<E, _Float16>::value;
+template <class E>
+constexpr float kLag = kLifted<E> ? 2.0f : 8.0f;
+template <class E>
+constexpr float kSumLift = kLifted<E> ? 13.0f : 0.0f;
+template <class E>
+constexpr float kSumDrop = kLifted<E> ? 0x1p-13f : 1.0f;
 
 // ---- a block of keys ----------------------------------------------------------------------------------
 //
 // 32 KT keys for the 32 rows of a wave: running maximum m and sum l (of the scores times c, to base 2) of the lane's row and the
-// transposed sums o.  key(n, i) and value(n, half, d) are the operands of 32 keys n, `hide` puts -inf in the place of scores that are not seen.
+// transposed sums o, both times 2^kSumLift.  key(n, i) and value(n, half, d) are the operands of 32 keys n, `hide` puts -inf in the place of scores that are not seen.
 template <class E, int WIDTH, int KT, class Key, class Value, class Hide>
 __device__ __forceinline__ void attend_to(Key key, Value value, const typename Operand<E>::type (&q)[WIDTH / 16], float c, float &m, float &l,
                                           v16f (&o)[WIDTH / 32], Hide hide)
@@ -398,8 +412,7 @@ __device__ __forceinline__ void attend_to(Key key, Value value, const typename O
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = __builtin_elementwise_maximum(most, x[n][i]);
     most = both_max(most) * c;
-    // The reference is raised only where a score passes it by 2^8: up to there sums and operands lose nothing.
-    if (__any(most > m + 8.0f)) {
+    if (__any(most > m + kLag<E>)) {
         const float next = most > m ? most : m, f = __builtin_amdgcn_exp2f(m - next);
         m = next;
         l *= f;
@@ -412,7 +425,7 @@ __device__ __forceinline__ void attend_to(Key key, Value value, const typename O
     for (int n = 0; n < KT; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, -m));
+            x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, kSumLift<E> - m));
             l += x[n][i];
         }
 #pragma unroll

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
             const int at = d * 32 + 8 * i + 4 * h;
             if (there && at < a.dim) store_side(op + at, v);
         }
-    if (a.lse && there && h == 0) a.lse[(int64_t)head * a.q_rows + s.q0 + row] = seen > 0 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (a.lse && there && h == 0) a.lse[(int64_t)head * a.q_rows + s.q0 + row] = seen > 0 ? (m + __builtin_amdgcn_logf(l * kSumDrop<E>)) * kLn2 : -INFINITY;
 
     uint64_t again = __ballot(bad && there);
     again = (again | again >> 32) & 0xffffffffu;
