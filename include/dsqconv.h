@@ -535,6 +535,8 @@ size_t dsq_attention_cache_bytes(int sequences, int max_rows, int q_heads, int k
  * The first rope_dim elements of a head are rotated (a multiple of 16, 0 for none), the others
  * pass.  Pair j is the elements j and j + rope_dim / 2, or 2j and 2j + 1 (interleaved != 0).
  * Angles are formed in binary64, everything else in binary32, rounded to dtype once.
+ * A head with an infinity (and no NaN) is normed to NaN there and to 0 elsewhere, before its rotation; a
+ * NaN makes its whole head NaN.  No other head is touched.
  *
  * q, k       device, heads; one may be NULL with 0 heads
  * v          device, [rows][kv_heads] heads that go to the cache as they are; else unused

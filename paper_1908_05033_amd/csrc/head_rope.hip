@@ -79,7 +79,8 @@ __device__ __forceinline__ double lanes_sum(double v)
     return v;
 }
 
-// 1 / rms of 16 elements a lane; squares in binary64, so nothing over- or underflows.
+// 1 / rms of 16 elements a lane; squares in binary64, so nothing over- or underflows.  0 for a head with an infinity (the step that makes
+// the reciprocal root exact would be infinity times zero): its finite elements are normed to 0.
 template <int LANES>
 __device__ __forceinline__ float rms_of(const float *x, int dim, float eps)
 {
@@ -88,7 +89,7 @@ __device__ __forceinline__ float rms_of(const float *x, int dim, float eps)
     for (int i = 0; i < 16; ++i) s = __builtin_fma((double)x[i], (double)x[i], s);
     const double mean = lanes_sum<LANES>(s) / dim + (double)eps;
     const double y = __builtin_amdgcn_rsq(mean);
-    return (float)(y * __builtin_fma(-0.5 * mean * y, y, 1.5));
+    return y == 0.0 ? 0.0f : (float)(y * __builtin_fma(-0.5 * mean * y, y, 1.5));
 }
 
 // Cosine and sine of the pairs of `count` rows from `row` on, 256 numbers a row.
