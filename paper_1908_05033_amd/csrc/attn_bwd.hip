@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 && ROW_WAVES == 4 ? 2 : 1) void
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
-    const int number = tile_of_turn(of, tiles, a.sequences);
+    const int number = attn_tile_of_turn(of, tiles, a.sequences);
     if (number < 0) return;
     const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, ROWS, number);
     if (s.at < 0) return;
@@ -364,30 +364,17 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(DsqAttnBwdArgs a, in
     }
 }
 
-// Rows times heads up to which the waves of the queries' kernel split the keys.  Both kernels together, us, 128 (binary32: 64) rows / 32
-// rows a workgroup:
-//
-//                   1024 x 8    2048 x 8    1024 x 32   2048 x 16   4096 x 8
-//   bfloat16, 128   63 / 57     97 / 93     76 / 111    107 / 147   186 / 236
-//   bfloat16, 64    45 / 39     68 / 57     54 / 58     74 / 75     129 / 121
-//   binary32, 128   183 / 145   397 / 338   335 / 391   599 / 669   1131 / 1225
-template <class E, int WIDTH>
-constexpr int64_t kFew = sizeof(E) == 2 && WIDTH == 64 ? 49152 : 32768;
-
-
-int tiles_of(const DsqAttnBwdArgs &a, int rows, int tile) { return a.q_starts ? rows / tile + a.sequences : (rows + tile - 1) / tile; }
-
 template <class E, int WIDTH, int ROW_WAVES>
 hipError_t queries(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
-    const int tiles = tiles_of(a, a.q_rows, 32 * ROW_WAVES);
-    attn_bwd_q_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)turns_of(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
+    const int tiles = attn_tiles(a.q_rows, 32 * ROW_WAVES, a.sequences, a.q_starts);
+    attn_bwd_q_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)attn_turns(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 template <class E, int WIDTH, int KEY_PAIRS, int ROW_PAIRS, int SUB>
 hipError_t keys(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
-    const int tiles = tiles_of(a, a.k_rows, 32 * KEY_PAIRS);
+    const int tiles = attn_tiles(a.k_rows, 32 * KEY_PAIRS, a.sequences, a.q_starts);
     const int64_t groups = (int64_t)tiles * a.kv_heads, each = (int64_t)a.k_rows * a.kv_heads * a.dim;
     // Workgroups for two rounds of the card, as far as there are rows and room.
     int64_t splits = 512 / groups;
@@ -405,15 +392,21 @@ template <class E, int WIDTH>
 hipError_t launch(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
     constexpr bool SINGLE = sizeof(E) == 4;
-    if (a.q_rows > 0)
-        if (const hipError_t e = (int64_t)a.q_rows * a.q_heads < kFew<E, WIDTH> ? queries<E, WIDTH, 1>(a, stream) : queries<E, WIDTH, SINGLE ? 2 : 4>(a, stream)) return e;
+    if (a.q_rows > 0) {
+        const bool few = attn_bwd_rows(sizeof(E), WIDTH, a.q_rows, a.q_heads) == 32;
+        if (const hipError_t e = few ? queries<E, WIDTH, 1>(a, stream) : queries<E, WIDTH, SINGLE ? 2 : 4>(a, stream)) return e;
+    }
     return a.k_rows > 0 ? keys<E, WIDTH, SINGLE ? 1 : 2, 2, 2>(a, stream) : hipSuccess;
 }
 
 template <class E>
 hipError_t of_dim(const DsqAttnBwdArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? launch<E, 64>(a, stream) : a.dim <= 96 ? launch<E, 96>(a, stream) : launch<E, 128>(a, stream);
+    switch (attn_width(a.dim)) {
+    case 64: return launch<E, 64>(a, stream);
+    case 96: return launch<E, 96>(a, stream);
+    default: return launch<E, 128>(a, stream);
+    }
 }
 
 }  // namespace

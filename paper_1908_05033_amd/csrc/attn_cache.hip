@@ -585,7 +585,11 @@ hipError_t launch(const DsqAttnCacheArgs &a, hipStream_t stream)
 template <class E>
 hipError_t of_dim(const DsqAttnCacheArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? launch<E, 64>(a, stream) : a.dim <= 96 ? launch<E, 96>(a, stream) : launch<E, 128>(a, stream);
+    switch (attn_width(a.dim)) {
+    case 64: return launch<E, 64>(a, stream);
+    case 96: return launch<E, 96>(a, stream);
+    default: return launch<E, 128>(a, stream);
+    }
 }
 
 }  // namespace

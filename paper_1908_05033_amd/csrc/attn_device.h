@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "attn_kernels.h"
+#include "attn_prompt_plan.h"
 #include "lm_device.h"
 
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -310,8 +311,7 @@ struct ColumnOperands {
 
 // ---- packed sequences ---------------------------------------------------------------------------
 //
-// Tiles of `tile` rows: sequence s has its own from number starts[s] / tile + s on, which leaves room for as many as it
-// needs without a sum over the sequences before it; tiles past its end have nothing to do.
+// How they number their tiles: attn_prompt_plan.h.
 struct Sequence {
     int at, q0, q_len, k0, k_len;            // at: the tile's first row within the sequence; negative: no tile
 };
@@ -326,21 +326,13 @@ __device__ __forceinline__ int find_sequence(const int32_t *starts, int rows, in
     int lo = 0, n = sequences;
     while (true) {
         const int step = (n + 63) / 64, s = lane * step < n ? lo + lane * step : lo, start = clamped(starts[s], rows);
-        const int count = __popcll(__ballot(lane * step < n && (tile ? start / tile + s : start) <= number));
+        const int count = __popcll(__ballot(lane * step < n && (tile ? attn_first_tile(start, tile, s) : start) <= number));
         if (count == 0) return -1;
         lo += (count - 1) * step;
         n = n - (count - 1) * step < step ? n - (count - 1) * step : step;
         if (n <= 1) return __builtin_amdgcn_readfirstlane(lo);
     }
 }
-
-// The tile that is the turn's: the last tiles of a causal prompt are the longest and go first, those of all sequences in turn.
-__device__ __forceinline__ int tile_of_turn(int turn, int tiles, int sequences)
-{
-    const int each = (tiles + sequences - 1) / sequences;
-    return tiles - 1 - turn % sequences * each - turn / sequences;
-}
-inline int turns_of(int tiles, int sequences) { return (tiles + sequences - 1) / sequences * sequences; }
 
 // by_keys: the tiles are of keys.
 __device__ __forceinline__ Sequence tile_of(const int32_t *q_starts, const int32_t *k_starts, int q_rows, int k_rows, int sequences,
@@ -360,7 +352,7 @@ __device__ __forceinline__ Sequence tile_of(const int32_t *q_starts, const int32
         s.k_len = clamped(k_starts[i + 1], k_rows) - s.k0;
         if (s.q_len < 0) s.q_len = 0;
         if (s.k_len < 0) s.k_len = 0;
-        s.at = (number - (by_keys ? s.k0 : s.q0) / tile - i) * tile;
+        s.at = (number - attn_first_tile(by_keys ? s.k0 : s.q0, tile, i)) * tile;
     }
     if (s.at >= (by_keys ? s.k_len : s.q_len)) s.at = -1;
     return s;

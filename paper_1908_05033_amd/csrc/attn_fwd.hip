@@ -30,16 +30,6 @@ struct Fwd {
     typedef Tile<E, HD> T;
 };
 
-// Rows times heads up to which waves split the keys: there 128 rows a workgroup leave compute units idle and make few long walks over the
-// keys.  Us, 128 rows / 32 rows a workgroup, rows x heads (causal):
-//
-//                   1024 x 8   2048 x 8   1024 x 32   2048 x 16   4096 x 8
-//   bfloat16, 128   22 / 16    41 / 33    24 / 45     42 / 65     77 / 103
-//   bfloat16, 64    19 / 11    34 / 19    19 / 19     34 / 25     62 / 40
-//   binary32, 128   144 / 55   284 / 114  146 / 140   284 / 228   559 / 406
-template <class E, int WIDTH>
-constexpr int64_t kFew = sizeof(E) == 2 && WIDTH > 64 ? 32768 : 49152;
-
 // Keys of one row of a packed prompt.
 template <class E>
 struct PromptKeys {
@@ -66,7 +56,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     const int of = blockIdx.x / a.q_heads, turn = blockIdx.x % a.q_heads;
     const int head = a.q_heads % 8 == 0 ? turn % 8 * (a.q_heads / 8) + turn / 8 : turn;
     const int kv = head / (a.q_heads / a.kv_heads);
-    const int number = tile_of_turn(of, tiles, a.sequences);
+    const int number = attn_tile_of_turn(of, tiles, a.sequences);
     if (number < 0) return;
     const Sequence s = tile_of(a.q_starts, a.k_starts, a.q_rows, a.k_rows, a.sequences, false, F::ROWS, number);
     if (s.at < 0) return;
@@ -206,21 +196,25 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
 template <class E, int WIDTH, int ROW_WAVES>
 hipError_t launch(const DsqAttnArgs &a, hipStream_t stream)
 {
-    const int rows = Fwd<E, WIDTH, ROW_WAVES>::ROWS, tiles = a.q_starts ? a.q_rows / rows + a.sequences : (a.q_rows + rows - 1) / rows;
-    attn_fwd_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)turns_of(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
+    const int rows = Fwd<E, WIDTH, ROW_WAVES>::ROWS, tiles = attn_tiles(a.q_rows, rows, a.sequences, a.q_starts);
+    attn_fwd_kernel<E, WIDTH, ROW_WAVES><<<(unsigned)((int64_t)attn_turns(tiles, a.sequences) * a.q_heads), 256, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }
 
 template <class E, int WIDTH>
 hipError_t of_rows(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return (int64_t)a.q_rows * a.q_heads < kFew<E, WIDTH> ? launch<E, WIDTH, 1>(a, stream) : launch<E, WIDTH, 4>(a, stream);
+    return attn_fwd_rows(sizeof(E), WIDTH, a.q_rows, a.q_heads) == 32 ? launch<E, WIDTH, 1>(a, stream) : launch<E, WIDTH, 4>(a, stream);
 }
 
 template <class E>
 hipError_t of_dim(const DsqAttnArgs &a, hipStream_t stream)
 {
-    return a.dim <= 64 ? of_rows<E, 64>(a, stream) : a.dim <= 96 ? of_rows<E, 96>(a, stream) : of_rows<E, 128>(a, stream);
+    switch (attn_width(a.dim)) {
+    case 64: return of_rows<E, 64>(a, stream);
+    case 96: return of_rows<E, 96>(a, stream);
+    default: return of_rows<E, 128>(a, stream);
+    }
 }
 
 }  // namespace
