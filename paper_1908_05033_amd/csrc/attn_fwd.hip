@@ -21,12 +21,14 @@ namespace {
 template <class E, int WIDTH, int ROW_WAVES>
 struct Fwd {
     static constexpr int SPLIT = 4 / ROW_WAVES, ROWS = 32 * ROW_WAVES, KT = SPLIT == 1 && sizeof(E) == 2 ? 2 : 1, KEYS = 32 * KT * SPLIT;
-    static constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32, TILE = KEYS * HD, BUFFERS = 4 * TILE * (int)sizeof(E) <= 131072 ? 2 : 1;
+    static constexpr int HD = kRow<WIDTH>, STEPS = WIDTH / 16, DT = WIDTH / 32, TILE = KEYS * HD;
     // binary32 keys that one wave reads alone need no LDS and no barriers: 6 % less time at 128 elements, 15 % at 96, but at 64 (where two
     // workgroups share a compute unit) 5 to 40 % more.
     static constexpr bool NEAR = sizeof(E) == 4 && ROW_WAVES == 1 && WIDTH > 64;
-    static constexpr int BYTES = most(NEAR ? 0 : BUFFERS * 2 * TILE * (int)sizeof(E), (SPLIT - 1) * ROW_WAVES * DT * 4096);
-    static constexpr bool DIRECT = sizeof(E) == 2 && BUFFERS == 2;
+    // Two buffers, each a tile of keys and one of values.
+    static constexpr int TILES = NEAR ? 0 : 4 * TILE * (int)sizeof(E), BYTES = most(TILES, (SPLIT - 1) * ROW_WAVES * DT * 4096);
+    static constexpr bool DIRECT = sizeof(E) == 2;
+    static_assert(TILES <= 131072, "tiles, and the waves' statistics beside them, fit the LDS of a compute unit");
     typedef Tile<E, HD> T;
 };
 
@@ -102,11 +104,10 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
     const auto block = [&](int t, auto buffer) {
         constexpr int B = decltype(buffer)::value;
         E *const kt = reinterpret_cast<E *>(room) + B * 2 * F::TILE, *const vt = kt + F::TILE;
-        if (F::BUFFERS == 1) __syncthreads();
         km.finish(kt);
         vm.finish(vt);
         __syncthreads();
-        if (t + 1 < count) start(t + 1, F::BUFFERS - 1 - B);
+        if (t + 1 < count) start(t + 1, 1 - B);
         const int at = t * F::KEYS + part * 32 * F::KT, in = part * 32 * F::KT;      // the wave's first key, and its place in the tile
         if (at < any)
             attend<E, WIDTH, F::KT>(kt, vt, in, q, c, m, l, o, lane, [&](v16f (&x)[F::KT]) { hide(x, at); });
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
         if (count > 0) start(0, 0);
         for (int t = 0; t < count; t += 2) {
             block(t, std::integral_constant<int, 0>());
-            if (t + 1 < count) block(t + 1, std::integral_constant<int, F::BUFFERS - 1>());
+            if (t + 1 < count) block(t + 1, std::integral_constant<int, 1>());
         }
     }
 
