@@ -16,8 +16,6 @@
 
 namespace {
 
-constexpr int kUnit = 128;                   // keys a chunk is a multiple of: a block for each wave
-
 __device__ __forceinline__ int sum_to(int v, int lane)
 {
     for (int off = 1; off < 64; off <<= 1) {
@@ -29,13 +27,12 @@ __device__ __forceinline__ int sum_to(int v, int lane)
 
 __device__ __forceinline__ int length_of(const DsqAttnCacheArgs &a, int s) { return clamped(a.lengths[s], a.table_pages << a.page_bits); }
 
-// Chunks have the same number of units for all sequences, and are numbered as tiles of sequences are: sequence s has them from (units
-// before it) / units a chunk + s on.  Finds the sequence of chunk `number`, or (`number` negative) takes the sequence s; returns
-// its first number, and the units of a chunk.  All 64 lanes take part; s is negative if there is none.
+// The sums over the sequences that chunks are numbered by (attn_cache_plan.h).  Finds the sequence of chunk `number`, or (`number`
+// negative) takes the sequence s; returns its first number, and the units of a chunk.  All 64 lanes take part; s is negative if there is none.
 __device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int slots, int number, int &s, int &units)
 {
     const int lane = threadIdx.x & 63;
-    const auto units_of = [&](int i) { return i < a.sequences ? (length_of(a, i) + kUnit - 1) / kUnit : 0; };
+    const auto units_of = [&](int i) { return i < a.sequences ? attn_units(length_of(a, i)) : 0; };
     const int head = units_of(lane), head_sum = sum_to(head, lane);      // (the first 64 are looked at once)
     int total = __shfl(head_sum, 63);
     if (a.sequences > 64) {
@@ -44,12 +41,11 @@ __device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int slots,
         for (int off = 32; off > 0; off >>= 1) more += __shfl_xor(more, off);
         total += more;
     }
-    units = (total + slots - 1) / slots;
-    units = units > 0 ? units : 1;
+    units = attn_chunk_units(total, slots);
     int before = 0, found = -1, at = -1;
     for (int base = 0; base < a.sequences; base += 64) {
         const int i = base + lane, mine = base ? units_of(i) : head, sum = base ? sum_to(mine, lane) : head_sum;
-        const int slot = (before + sum - mine) / units + i;
+        const int slot = attn_first_chunk(before + sum - mine, units, i);
         const uint64_t ok = __ballot(i < a.sequences && (number < 0 ? i <= s : slot <= number));
         if (ok == 0) break;
         const int last = 63 - __clzll((long long)ok);
@@ -62,9 +58,6 @@ __device__ __forceinline__ int first_chunk(const DsqAttnCacheArgs &a, int slots,
     units = __builtin_amdgcn_readfirstlane(units);
     return __builtin_amdgcn_readfirstlane(at);
 }
-
-// Keys of a chunk of so many units: a sequence has at most 2^30.
-__device__ __forceinline__ int chunk_keys(int units) { return (units < 1 << 23 ? units : 1 << 23) * kUnit; }
 
 // Where key j of a sequence lies: a row of [pages][kv heads][page], negative where there is none.
 struct Pages {
@@ -139,7 +132,7 @@ struct Work {
         int units;
         const int slot0 = first_chunk(a, slots, number, s, units);
         if (s < 0) return false;
-        const int chunk = chunk_keys(units);
+        const int chunk = attn_chunk_keys(units);
         of_sequence(a);
         if ((int64_t)(number - slot0) * chunk >= length && number != slot0) return false;
         first = (number - slot0) * chunk;
@@ -493,7 +486,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
     int of = s;
     const int slot0 = first_chunk(a, slots, -1, of, units);
     const int t0 = a.q_starts ? clamped(a.q_starts[s], a.rows) : s, tokens = a.q_starts ? clamped(a.q_starts[s + 1], a.rows) - t0 : 1;
-    const int length = length_of(a, s), chunk = chunk_keys(units), chunks = (int)(((int64_t)length + chunk - 1) / chunk);
+    const int length = length_of(a, s), chunk = attn_chunk_keys(units), chunks = (int)(((int64_t)length + chunk - 1) / chunk);
     if (t < t0 || t - t0 >= tokens || t - t0 >= a.max_rows || chunks <= 1) return;
     const int64_t step = (int64_t)a.kv_heads * most_rows * a.dim;
     const int d0 = lane < a.dim ? lane : 0, d1 = lane + 64 < a.dim ? lane + 64 : 0;
@@ -573,12 +566,13 @@ hipError_t launch(const DsqAttnCacheArgs &a, hipStream_t stream)
     else if (p.single) attn_cache_kernel<E, WIDTH, sizeof(E) == 2 ? 8 : 4><<<groups, sizeof(E) == 2 ? 512 : 256, 0, stream>>>(a, p.slots);
     else attn_cache_kernel<E, WIDTH, 4><<<groups, 256, 0, stream>>>(a, p.slots);
     if (const hipError_t e = hipGetLastError()) return e;
-    if (p.single) return hipSuccess;
-    // Many chunks a row: a workgroup of 16 waves each; a few: a wave takes one row, or four where there are many.
     const int64_t rows = (int64_t)a.rows * a.q_heads, fours = (int64_t)a.rows * ((a.q_heads + 3) / 4);
-    if (p.slots / a.sequences >= 16 && rows <= 1024) attn_cache_join_kernel<E, 16, 1><<<(unsigned)rows, 1024, 0, stream>>>(a, p.slots);
-    else if (rows <= 4096) attn_cache_join_kernel<E, 1, 1><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a, p.slots);
-    else attn_cache_join_kernel<E, 1, 4><<<(unsigned)((fours + 3) / 4), 256, 0, stream>>>(a, p.slots);
+    switch (attn_cache_join(p, a.rows, a.q_heads, a.sequences)) {
+    case kJoinNone: break;
+    case kJoinSixteen: attn_cache_join_kernel<E, 16, 1><<<(unsigned)rows, 1024, 0, stream>>>(a, p.slots); break;
+    case kJoinOne: attn_cache_join_kernel<E, 1, 1><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a, p.slots); break;
+    case kJoinFour: attn_cache_join_kernel<E, 1, 4><<<(unsigned)((fours + 3) / 4), 256, 0, stream>>>(a, p.slots); break;
+    }
     return hipGetLastError();
 }
 
