@@ -102,9 +102,9 @@ struct CacheKeys {
     Tree tree;
     int first, n, dim;
     __device__ int count() const { return n; }
-    __device__ bool seen(int j) const { return pages.row(first + j) >= 0 && (tree.mask(first + j) & 1); }
-    __device__ const E *key(int j) const { return k + pages.row(first + j) * dim; }
-    __device__ const E *value(int j) const { return v + pages.row(first + j) * dim; }
+    __device__ int64_t place(int j) const { return tree.mask(first + j) & 1 ? pages.row(first + j) : -1; }
+    __device__ const E *key(int64_t place) const { return k + place * dim; }
+    __device__ const E *value(int64_t place) const { return v + place * dim; }
 };
 
 // What a workgroup has to do: a chunk of a sequence's keys for a key head.
@@ -151,11 +151,11 @@ __device__ __forceinline__ float *logs_of(const DsqAttnCacheArgs &a, int slots, 
 
 // A finished row (its logarithm to base 2, normed elements lane and lane + 64 of a wave): to the output, or to where chunks are joined.
 template <class E>
-__device__ __forceinline__ void leave_row(const DsqAttnCacheArgs &a, const Work &w, int slots, int number, int kv, int of, bool seen, float log2, const float y[2])
+__device__ __forceinline__ void leave_row(const DsqAttnCacheArgs &a, const Work &w, int slots, int number, int kv, int of, int token, bool seen, float log2, const float y[2])
 {
     const int lane = threadIdx.x & 63, group = a.q_heads / a.kv_heads, most_rows = a.max_rows * group;
     if (w.whole) {
-        E *to = (E *)a.out.p + (int64_t)(w.t0 + of / group) * a.out.row + (kv * group + of % group) * a.out.head;
+        E *to = (E *)a.out.p + (int64_t)(w.t0 + token) * a.out.row + (kv * group + of - token * group) * a.out.head;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
             if (lane + 64 * e < a.dim) to[lane + 64 * e] = (E)y[e];
@@ -170,13 +170,19 @@ __device__ __forceinline__ void leave_row(const DsqAttnCacheArgs &a, const Work 
     if (lane == 0) logs_of(a, slots, kv, of)[number] = seen ? log2 : -INFINITY;
 }
 
+// The keys of a chunk that a token sees.
 template <class E>
-__device__ __forceinline__ float again(const DsqAttnCacheArgs &a, const Work &w, const Pages &pages, int kv, int of, float c, float y[2])
+__device__ __forceinline__ CacheKeys<E> keys_of(const DsqAttnCacheArgs &a, const Work &w, const Pages &pages, int token)
 {
-    const int group = a.q_heads / a.kv_heads, token = of / group;
     const Tree its = {a.tree ? a.tree + (int64_t)(w.t0 + token) * a.tree_words : nullptr, a.tree_words, token, w.length - w.tokens};
-    const CacheKeys<E> keys = {(const E *)a.k_cache, (const E *)a.v_cache, pages, its, w.first, w.end - w.first, a.dim};
-    return row_again<E>((const E *)a.q.p + (int64_t)(w.t0 + token) * a.q.row + (kv * group + of % group) * a.q.head, a.dim, c, keys, y);
+    return {(const E *)a.k_cache, (const E *)a.v_cache, pages, its, w.first, w.end - w.first, a.dim};
+}
+
+template <class E>
+__device__ __forceinline__ float again(const DsqAttnCacheArgs &a, const Work &w, const CacheKeys<E> &keys, int kv, int of, int token, float c, float y[2])
+{
+    const int head = kv * (a.q_heads / a.kv_heads) + of - token * (a.q_heads / a.kv_heads);
+    return row_again<E>((const E *)a.q.p + (int64_t)(w.t0 + token) * a.q.row + head * a.q.head, a.dim, c, keys, y);
 }
 
 // Puts -inf in the place of the scores of 32 keys whose bit is not set.
@@ -305,8 +311,16 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 2 ? 2 : 1) void attn_cache
             bad |= !is_finite(y[e]);
         }
         float log2 = top + __builtin_amdgcn_logf(sum * kSumDrop<E>);
-        if (__any(bad)) log2 = again<E>(a, w, pages, kv, i, c, y);
-        leave_row<E>(a, w, slots, number, kv, i, seen != 0, log2, y);
+        if (__builtin_expect(__any(bad) && is_finite(sum), 0)) {
+            const CacheKeys<E> keys = keys_of<E>(a, w, pages, i / group);
+            const Spoilt its = spoilt_of(y[0], y[1]);
+            float z[2] = {0.0f, 0.0f};
+            if (!its.explained_by(add_spoilt<E>(keys, 0, a.dim, its, z))) {
+                if (stands_for(z, its)) y[0] = is_finite(z[0]) ? y[0] : z[0], y[1] = is_finite(z[1]) ? y[1] : z[1];
+                else log2 = again<E>(a, w, keys, kv, i, i / group, c, y);
+            }
+        }
+        leave_row<E>(a, w, slots, number, kv, i, i / group, seen != 0, log2, y);
     }
 }
 
@@ -426,7 +440,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
     float *mine_o = reinterpret_cast<float *>(&tiles_at[0][0][0]) + wave * TILE * (int)sizeof(E) / 4;
     l = both_sum(l);
     const float inv = any ? 1.0f / l : 0.0f, log2 = m + __builtin_amdgcn_logf(l * kSumDrop<E>);
-    bool bad = false;
+    float probe = 0.0f;                      // NaN once an element is not finite
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -434,16 +448,18 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
             v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
             if (any) y = v4f{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * inv;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) bad |= !is_finite(y[e]);
+            for (int e = 0; e < 4; ++e) probe = __builtin_fmaf(y[e], 0.0f, probe);
             *reinterpret_cast<v4f *>(mine_o + r * HD + ((d * 8 + 2 * i + h) ^ (r % (HD / 4))) * 4) = y;
         }
     wave_order();
     const int most_rows = a.max_rows * group;
     const int64_t rows_at = ((int64_t)number * a.kv_heads + kv) * most_rows + row0;
     constexpr int ACROSS = HD / 4, DOWN = 64 / ACROSS;          // lanes of a row, rows of a step
+    int of_lane = lane;
+    asm volatile("" : "+v"(of_lane));        // (its rows' numbers are not kept from before the loop, whose registers are full)
 #pragma unroll
     for (int i = 0; i < 32; i += DOWN) {
-        const int its = i + lane / ACROSS, at = lane % ACROSS;
+        const int its = i + of_lane / ACROSS, at = of_lane % ACROSS;
         const v4f y = *reinterpret_cast<const v4f *>(mine_o + its * HD + (at ^ (its % (HD / 4))) * 4);
         const int of = row0 + its;
         if (of >= w.mine * group || at * 4 >= a.dim) continue;
@@ -457,14 +473,27 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
         }
     }
     if (!w.whole && there && h == 0) logs_of(a, slots, kv, row)[number] = any ? log2 > kNoKey || log2 != log2 ? log2 : kNoKey : -INFINITY;
-    uint64_t spoilt = __ballot(bad && there);
-    spoilt = (spoilt | spoilt >> 32) & 0xffffffffu;
-    while (spoilt) {
-        const int i = __ffsll((unsigned long long)spoilt) - 1;
-        spoilt &= spoilt - 1;
+    // (rows whose sum is not finite see a score that is none; the keys before the drafted ones are seen by all)
+    const uint64_t asks = __ballot(probe != 0.0f && there && is_finite(l));
+    if (__builtin_expect(asks == 0, 1)) return;
+    const int before = w.length - w.tokens - w.first, keys = w.end - w.first;
+    const auto token_of = [&](int i) { return __builtin_amdgcn_readlane(token, i); };
+    const auto keys_of_row = [&](int i) { return keys_of<E>(a, w, pages, token_of(i)); };
+    const auto row_of = [&](int i, float (&y)[2]) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int d = of_lane + 64 * e;
+            y[e] = d < a.dim ? mine_o[i * HD + ((d / 4) ^ (i % (HD / 4))) * 4 + d % 4] : 0.0f;
+        }
+    };
+    uint32_t rows = rows_to_form<E>((uint32_t)(asks | asks >> 32), a.dim, before < 0 ? 0 : before < keys ? before : keys, row_of, keys_of_row,
+                                    [&](int i, const float (&y)[2]) { leave_row<E>(a, w, slots, number, kv, row0 + i, token_of(i), true, lanes_number(log2, i), y); });
+    while (rows) {
+        const int i = __ffs(rows) - 1;
+        rows &= rows - 1;
         float y[2];
-        const float its = again<E>(a, w, pages, kv, row0 + i, c, y);
-        leave_row<E>(a, w, slots, number, kv, row0 + i, true, its, y);
+        const float its = again<E>(a, w, keys_of_row(i), kv, row0 + i, token_of(i), c, y);
+        leave_row<E>(a, w, slots, number, kv, row0 + i, token_of(i), true, its, y);
     }
 }
 

@@ -413,11 +413,12 @@ __device__ __forceinline__ void attend_to(Key key, Value value, const typename O
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] *= f;
     }
+    const float ref = kLifted<E> ? kSumLift<E> - m : -m;
 #pragma unroll
     for (int n = 0; n < KT; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, kSumLift<E> - m));
+            x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, ref));
             l += x[n][i];
         }
 #pragma unroll
@@ -440,44 +441,197 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
                             [=](int n, int half, int d) { return T::column_operand(vt, in + n * 32 + half * 16, d * 32, lane); }, q, c, m, l, o, hide);
 }
 
-// ---- a row formed again ---------------------------------------------------------------------------
+// ---- rows that are not finite ---------------------------------------------------------------------
 //
-// A masked key counts for nothing, but in a product of whole tiles its zero meets its value, and zero times an infinity or
-// NaN is NaN.  Rows whose result is not finite are therefore formed again from their visible keys alone, by one wave each.
-// Keys: `int count()`, `bool seen(j)`, `const E *key(j)`, `const E *value(j)` for keys that are seen.
-// Leaves the normed row in o (elements lane, lane + 64 of it) and returns the logarithm to base 2 of its sum.
+// A key that a row does not see counts for nothing, but in a product of whole tiles its zero meets its value, and zero times an infinity or
+// NaN is NaN; and sums of values near the end of binary32 may pass it on the way.  Most rows that are not finite are so because of what they see, and an
+// infinity or NaN early in a sequence is seen by all rows after it, so a row is looked at in three steps:
+//   - the sum of its softmax is not finite: it sees a score that is NaN or plus infinity (hidden keys have no part in the sum), and nothing of it is finite;
+//   - each of its elements that is not finite sees a value that is not: the sum of those, infinity or NaN, is the element;
+//   - else the row is formed again from the keys it sees alone, by one wave: 2 to 4 ms for a row of 16384 keys.  In a causal prompt those are at most 63 rows
+//     a head for each value that is not finite (the ones before it in its tile), and the rows whose sums pass binary32.
+// Keys: `int count()`, `int64_t place(j)` of key j, negative if it is not seen, `const E *key(place)`, `const E *value(place)`.
+
+// Elements of a head, bit d % 64 of word d / 64: NaN, and infinities.
+struct Spoilt {
+    uint64_t nan[2], inf[2];
+    __device__ __forceinline__ bool explained_by(const Spoilt &v) const
+    {
+        return !((nan[0] & ~v.nan[0]) | (nan[1] & ~v.nan[1]) | (inf[0] & ~v.inf[0]) | (inf[1] & ~v.inf[1]));
+    }
+};
+// Of the elements lane and lane + 64 of all lanes.
+__device__ __forceinline__ Spoilt spoilt_of(float y0, float y1)
+{
+    return {{__ballot(y0 != y0), __ballot(y1 != y1)}, {__ballot(__builtin_fabsf(y0) == INFINITY), __ballot(__builtin_fabsf(y1) == INFINITY)}};
+}
+
+// Lane i's number, known to be the same for all lanes.
+__device__ __forceinline__ float lanes_number(float v, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), i)); }
+__device__ __forceinline__ int64_t lanes_number(int64_t v, int i)
+{
+    return (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+}
+
+// The keys at a wave's 64 places (negative: not seen), kAtOnce at a time, while take(places at(i), i = 0 .. kAtOnce - 1, bits of those that are seen) says so.
+// The place of one that is seen stands for one that is not.
+constexpr int kAtOnce = 8;
+template <class Take>
+__device__ __forceinline__ void seen_keys(int64_t place, Take take)
+{
+    const uint64_t seen = __ballot(place >= 0);
+    const int other = __ffsll((unsigned long long)seen) - 1;
+#pragma unroll 1
+    for (int i0 = 0; i0 < 64; i0 += kAtOnce) {
+        const uint32_t mask = (uint32_t)(seen >> i0) & ((1u << kAtOnce) - 1);
+        if (mask && !take([&](int i) { return lanes_number(place, mask >> i & 1 ? i0 + i : other); }, mask)) return;
+    }
+}
+// Elements lane and lane + 64 of kAtOnce vectors, zeros past a head's last.
+template <class E>
+struct AtOnce {
+    float low[kAtOnce], high[kAtOnce];
+    template <class Vector>
+    __device__ __forceinline__ void load(Vector vector, int dim)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const E *p = vector(i);
+            low[i] = (float)p[lane < dim ? lane : 0], high[i] = (float)p[lane + 64 < dim ? lane + 64 : 0];
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) low[i] = lane < dim ? low[i] : 0.0f, high[i] = lane + 64 < dim ? high[i] : 0.0f;
+    }
+};
+
+// Adds to y (elements lane and lane + 64) what is not finite in the values of the keys from `from` on, until that explains `wanted`.  All lanes take part.
+template <class E, class Keys>
+__device__ __forceinline__ Spoilt add_spoilt(const Keys &keys, int from, int dim, const Spoilt &wanted, float (&y)[2])
+{
+    const int lane = threadIdx.x & 63, count = keys.count();
+    Spoilt found = spoilt_of(y[0], y[1]);
+#pragma unroll 1
+    for (int j0 = from; j0 < count && !wanted.explained_by(found); j0 += 64) {
+        seen_keys(j0 + lane < count ? keys.place(j0 + lane) : -1, [&](auto at, uint32_t) {
+            AtOnce<E> v;
+            v.load([&](int i) { return keys.value(at(i)); }, dim);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                y[0] += is_finite(v.low[i]) ? 0.0f : v.low[i];
+                y[1] += is_finite(v.high[i]) ? 0.0f : v.high[i];
+            }
+            return true;
+        });
+        found = spoilt_of(y[0], y[1]);
+    }
+    return found;
+}
+// Do the values `z` that are not finite stand for all elements that are not?
+__device__ __forceinline__ bool stands_for(const float (&z)[2], const Spoilt &its)
+{
+    const int lane = threadIdx.x & 63;
+    return !__any(((its.nan[0] | its.inf[0]) >> lane & 1 && is_finite(z[0])) || ((its.nan[1] | its.inf[1]) >> lane & 1 && is_finite(z[1])));
+}
+
+// Is there a NaN in the keys?
+template <class E, class Keys>
+__device__ __forceinline__ bool nan_among(const Keys &keys, int dim)
+{
+    const int lane = threadIdx.x & 63, count = keys.count();
+    bool found = false;
+#pragma unroll 1
+    for (int j0 = 0; j0 < count && !__any(found); j0 += 64)
+        seen_keys(j0 + lane < count ? keys.place(j0 + lane) : -1, [&](auto at, uint32_t) {
+            AtOnce<E> k;
+            k.load([&](int i) { return keys.key(at(i)); }, dim);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) found |= k.low[i] != k.low[i] || k.high[i] != k.high[i];
+            return true;
+        });
+    return __any(found);
+}
+
+// Which of a wave's `rows` (bit r: row r) have to be formed again.  row_of(r, y): the row's elements lane and lane + 64; keys_of(r): its keys, of which
+// all of these rows see the first `common`.  Of the other rows put(r, y) stores those in whose place there is something else.
+template <class E, class RowOf, class KeysOf, class Put>
+__device__ __forceinline__ uint32_t rows_to_form(uint32_t rows, int dim, int common, RowOf row_of, KeysOf keys_of, Put put)
+{
+    uint32_t again = 0;
+    Spoilt wanted = {{0, 0}, {0, 0}};
+    for (uint32_t left = rows; left; left &= left - 1) {
+        float y[2];
+        row_of(__ffs(left) - 1, y);
+        const Spoilt its = spoilt_of(y[0], y[1]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) wanted.nan[e] |= its.nan[e], wanted.inf[e] |= its.inf[e];
+    }
+    auto shared = keys_of(__ffs(rows) - 1);
+    shared.n = common;
+    float sum[2] = {0.0f, 0.0f};
+    const Spoilt found = add_spoilt<E>(shared, 0, dim, wanted, sum);
+    for (uint32_t left = rows; left; left &= left - 1) {
+        const int i = __ffs(left) - 1;
+        float y[2], z[2] = {sum[0], sum[1]};
+        row_of(i, y);
+        const Spoilt its = spoilt_of(y[0], y[1]);
+        if (its.explained_by(found)) continue;
+        add_spoilt<E>(keys_of(i), common, dim, {{~0ull, ~0ull}, {0, 0}}, z);
+        if (!stands_for(z, its)) {
+            again |= 1u << i;
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) y[e] = is_finite(z[e]) ? y[e] : z[e];
+        put(i, y);
+    }
+    return again;
+}
+
+// Leaves the normed row in o (elements lane, lane + 64 of it) and returns the logarithm to base 2 of its sum.  One pass over the keys; o is a
+// mean of the values so far at any time, so no sum passes the largest of them.
 template <class E, class Keys>
 __device__ __forceinline__ float row_again(const E *q, int dim, float c, const Keys &keys, float o[2])
 {
     const int lane = threadIdx.x & 63, count = keys.count();
-    auto score = [&](int j) {
-        const E *k = keys.key(j);
-        float s = 0.0f;
-        for (int d = 0; d < dim; ++d) s = __builtin_fmaf((float)q[d], (float)k[d], s);
-        return s * c;
-    };
-    float m = kNoKey;
-    for (int j = lane; j < count; j += 64)
-        if (keys.seen(j)) m = __builtin_elementwise_maximum(m, score(j));
-    for (int off = 32; off > 0; off >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, off));
-    float l = 0.0f;
-    for (int j = lane; j < count; j += 64)
-        if (keys.seen(j)) l += __builtin_amdgcn_exp2f(score(j) - m);
-    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+    const float q0 = lane < dim ? (float)q[lane] : 0.0f, q1 = lane + 64 < dim ? (float)q[lane + 64] : 0.0f;
+    float m = kNoKey, l = 0.0f;
     o[0] = o[1] = 0.0f;
-    for (int j0 = 0; j0 < count; j0 += 64) {
-        const int mine = j0 + lane;
-        const bool seen = mine < count && keys.seen(mine);
-        const float p = seen ? __builtin_amdgcn_exp2f(score(mine) - m) / l : 0.0f;
-        uint64_t left = __ballot(seen);
-        while (left) {
-            const int i = __ffsll((unsigned long long)left) - 1;
-            left &= left - 1;
-            const float pi = __shfl(p, i);
-            const E *v = keys.value(j0 + i);
-            if (lane < dim) o[0] = __builtin_fmaf(pi, (float)v[lane], o[0]);
-            if (lane + 64 < dim) o[1] = __builtin_fmaf(pi, (float)v[lane + 64], o[1]);
-        }
-    }
+#pragma unroll 1
+    for (int j0 = 0; j0 < count && m < INFINITY; j0 += 64)
+        seen_keys(j0 + lane < count ? keys.place(j0 + lane) : -1, [&](auto at, uint32_t mask) {
+            AtOnce<E> k, v;
+            k.load([&](int i) { return keys.key(at(i)); }, dim);
+            v.load([&](int i) { return keys.value(at(i)); }, dim);
+            float s[kAtOnce], top = m, sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) s[i] = __builtin_fmaf(q0, k.low[i], q1 * k.high[i]);
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1)
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) s[i] += __shfl_xor(s[i], off);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                s[i] = mask >> i & 1 ? s[i] * c : -INFINITY;
+                top = __builtin_elementwise_maximum(top, s[i]);
+            }
+            const float before = l * __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - top), sum += s[i];
+            m = top;
+            l = before + sum;
+            if (!(m < INFINITY)) return false;
+            if (l == 0.0f) return true;                          // (scores of minus infinity alone)
+            const float by = 1.0f / l;
+            o[0] *= before * by, o[1] *= before * by;
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                o[0] = mask >> i & 1 ? __builtin_fmaf(s[i] * by, v.low[i], o[0]) : o[0];
+                o[1] = mask >> i & 1 ? __builtin_fmaf(s[i] * by, v.high[i], o[1]) : o[1];
+            }
+            return true;
+        });
+    // (a score of NaN or plus infinity: nothing of the row is finite; no sum: neither)
+    if (!(m < INFINITY) || l == 0.0f) o[0] = o[1] = __builtin_nanf("");
     return m + __builtin_amdgcn_logf(l);
 }

@@ -39,9 +39,9 @@ struct PromptKeys {
     int64_t k_row, v_row;
     int n;
     __device__ int count() const { return n; }
-    __device__ bool seen(int) const { return true; }
-    __device__ const E *key(int j) const { return k + j * k_row; }
-    __device__ const E *value(int j) const { return v + j * v_row; }
+    __device__ int64_t place(int j) const { return j; }
+    __device__ const E *key(int64_t j) const { return k + j * k_row; }
+    __device__ const E *value(int64_t j) const { return v + j * v_row; }
 };
 
 template <class E, int WIDTH, int ROW_WAVES>
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
         for (int p = 0; p < F::SPLIT; ++p) l += stat[1][p][mine];
     }
     const float inv = seen > 0 ? 1.0f / l : 0.0f;
-    bool bad = false;
+    float probe = 0.0f;                      // NaN once an element is not finite
     E *op = (E *)a.out.p + (int64_t)(s.q0 + row) * a.out.row + head * a.out.head;
 #pragma unroll
     for (int d = 0; d < F::DT; ++d)
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float y = seen > 0 ? o[d][4 * i + e] * inv : 0.0f;
-                bad |= !is_finite(y);
+                probe = __builtin_fmaf(y, 0.0f, probe);
                 v.at[e] = (E)y;
             }
             const int at = d * 32 + 8 * i + 4 * h;
@@ -179,18 +179,42 @@ __global__ __launch_bounds__(256, ROW_WAVES == 4 && (sizeof(E) == 2 || WIDTH == 
         }
     if (a.lse && there && h == 0) a.lse[(int64_t)head * a.q_rows + s.q0 + row] = seen > 0 ? (m + __builtin_amdgcn_logf(l * kSumDrop<E>)) * kLn2 : -INFINITY;
 
-    uint64_t again = __ballot(bad && there);
-    again = (again | again >> 32) & 0xffffffffu;
-    while (again) {
-        const int i = __ffsll((unsigned long long)again) - 1, at = first_row + i;
-        again &= again - 1;
-        const PromptKeys<E> keys = {kp, vp, a.k.row, a.v.row, visible(s, a.causal, at)};
-        float y[2];
-        const float log2 = row_again<E>((const E *)a.q.p + (int64_t)(s.q0 + at) * a.q.row + head * a.q.head, a.dim, c, keys, y);
-        E *to = (E *)a.out.p + (int64_t)(s.q0 + at) * a.out.row + head * a.out.head;
+    // (attn_device.h: rows that are not finite.)
+    const bool asks = probe != 0.0f && there, odd = !is_finite(l);
+    if (__builtin_expect(!__any(asks), 1)) return;
+    const auto rows_of = [](uint64_t lanes) { return (uint32_t)(lanes | lanes >> 32); };
+    const auto keys_of = [&](int i) { return PromptKeys<E>{kp, vp, a.k.row, a.v.row, visible(s, a.causal, first_row + i)}; };
+    const auto query_of = [&](int i) { return (const E *)a.q.p + (int64_t)(s.q0 + first_row + i) * a.q.row + head * a.q.head; };
+    const auto out_of = [&](int i) { return (E *)a.out.p + (int64_t)(s.q0 + first_row + i) * a.out.row + head * a.out.head; };
+    uint32_t again = a.dim < WIDTH ? rows_of(__ballot(asks && odd)) : 0;
+    if (again) {
+        // Elements past a head's are its first ones again, so a key's minus infinity, a score like others, became NaN there.  A NaN in a key that all these rows
+        // see explains them; a row with one in its query ends at its first keys.
+        const int first = __ffs(again) - 1;
+        AtOnce<E> query;
+        query.load([&](int) { return query_of(first); }, a.dim);
+        if (!__any(query.low[0] != query.low[0] || query.high[0] != query.high[0]) && nan_among<E>(keys_of(first), a.dim)) again = 0;
+    }
+    const auto put = [&](int i, const float (&y)[2]) {
+        E *to = out_of(i);
         if (lane < a.dim) to[lane] = (E)y[0];
         if (lane + 64 < a.dim) to[lane + 64] = (E)y[1];
-        if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + s.q0 + at] = log2 * kLn2;
+    };
+    if (const uint32_t rows = rows_of(__ballot(asks && !odd))) {
+        __threadfence_block();                                   // (lanes read what others of the wave have stored)
+        const auto row_of = [&](int i, float (&y)[2]) {
+            const E *from = out_of(i);
+            y[0] = lane < a.dim ? (float)from[lane] : 0.0f, y[1] = lane + 64 < a.dim ? (float)from[lane + 64] : 0.0f;
+        };
+        again |= rows_to_form<E>(rows, a.dim, keys_of(__ffs(rows) - 1).n, row_of, keys_of, put);
+    }
+    while (again) {
+        const int i = __ffs(again) - 1;
+        again &= again - 1;
+        float y[2];
+        const float log2 = row_again<E>(query_of(i), a.dim, c, keys_of(i), y);
+        put(i, y);
+        if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + s.q0 + first_row + i] = log2 * kLn2;
     }
 }
 
