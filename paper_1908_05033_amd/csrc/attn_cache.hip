@@ -497,7 +497,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void attn_cache_tiles_
     }
 }
 
-// The chunks of a row, weighted by their sums.  WAVES waves take the chunks of a row in turn, or (WAVES = 1) a wave takes HEADS heads at once.
+// The chunks of a row, weighted by their shares of its sum (before they are added: values near the end of binary32 stay inside it).  WAVES
+// waves take the chunks of a row in turn, or (WAVES = 1) a wave takes HEADS heads at once.
 template <class E, int WAVES, int HEADS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join_kernel(DsqAttnCacheArgs a, int slots)
 {
@@ -520,14 +521,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
     const int64_t step = (int64_t)a.kv_heads * most_rows * a.dim;
     const int d0 = lane < a.dim ? lane : 0, d1 = lane + 64 < a.dim ? lane + 64 : 0;
     const float *logs[HEADS], *rows[HEADS];
-    float top[HEADS], y0[HEADS], y1[HEADS], sum[HEADS];
+    float top[HEADS], y0[HEADS], y1[HEADS], by[HEADS];
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
         const int head = head0 + i < a.q_heads ? head0 + i : a.q_heads - 1, row = (t - t0) * group + head % group;
         logs[i] = logs_of(a, slots, head / group, row) + slot0;
         rows[i] = a.partial + slot0 * step + ((int64_t)(head / group) * most_rows + row) * a.dim;
         top[i] = -INFINITY;
-        y0[i] = y1[i] = sum[i] = 0.0f;
+        y0[i] = y1[i] = by[i] = 0.0f;
     }
     for (int c = 0; c < chunks; c += 64)
 #pragma unroll
@@ -537,14 +538,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
         for (int off = 32; off > 0; off >>= 1) top[i] = __builtin_elementwise_maximum(top[i], __shfl_xor(top[i], off));
         top[i] = top[i] == -INFINITY ? 0.0f : top[i];            // (no chunk has a key that the row sees: all weights are zero)
     }
+    for (int c = 0; c < chunks; c += 64)
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) by[i] += c + lane < chunks ? __builtin_amdgcn_exp2f(logs[i][c + lane] - top[i]) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        for (int off = 32; off > 0; off >>= 1) by[i] += __shfl_xor(by[i], off);
+        by[i] = by[i] == 0.0f ? 0.0f : 1.0f / by[i];
+    }
     for (int base = 0; base < chunks; base += 64) {
         float f[HEADS];
         const int n = chunks - base < 64 ? chunks - base : 64;
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            f[i] = lane < n ? __builtin_amdgcn_exp2f(logs[i][base + lane] - top[i]) : 0.0f;
-            sum[i] += f[i];
-        }
+        for (int i = 0; i < HEADS; ++i) f[i] = lane < n ? __builtin_amdgcn_exp2f(logs[i][base + lane] - top[i]) * by[i] : 0.0f;
         for (int c0 = turn; c0 < n; c0 += AT_ONCE * WAVES) {
             // (loads of several chunks under way; those past the last have no weight)
             float v0[AT_ONCE][HEADS], v1[AT_ONCE][HEADS];
@@ -565,9 +571,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
                 }
         }
     }
-#pragma unroll
-    for (int i = 0; i < HEADS; ++i)
-        for (int off = 32; off > 0; off >>= 1) sum[i] += __shfl_xor(sum[i], off);
     if (WAVES > 1) {
         part[wave][lane] = y0[0];
         part[wave][lane + 64] = y1[0];
@@ -581,8 +584,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void attn_cache_join
     for (int i = 0; i < HEADS; ++i) {
         if (head0 + i >= a.q_heads) return;
         E *to = (E *)a.out.p + (int64_t)t * a.out.row + (head0 + i) * a.out.head;
-        if (lane < a.dim) to[lane] = (E)(sum[i] == 0.0f ? 0.0f : y0[i] / sum[i]);
-        if (lane + 64 < a.dim) to[lane + 64] = (E)(sum[i] == 0.0f ? 0.0f : y1[i] / sum[i]);
+        if (lane < a.dim) to[lane] = (E)y0[i];
+        if (lane + 64 < a.dim) to[lane + 64] = (E)y1[i];
     }
 }
 

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from heads_helpers import B, DTYPES
+from heads_helpers import B, DTYPES, half_step
+from lm_helpers import U32
 from test_gpu_attention_cache import Case
 
 pytestmark = pytest.mark.gpu
@@ -85,3 +86,15 @@ def test_heads_that_are_no_multiple_of_four(name, dtype):
     c.out = room[:, :c.hq]
     c.run()
     assert torch.equal(c.out, want) and (room[:, c.hq:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["one long", "tokens", "trees", "short trees", "two tiles"])
+def test_values_near_the_end_of_binary32(name, dtype):
+    """Chunks whose weighted sum would pass binary32 before it is divided; the result, a mean of equal values, is one of them."""
+    c = Case(7, dtype, *SHAPES[name])
+    c.cache[1].copy_(torch.where(torch.isnan(c.cache[1]), c.cache[1], 3e38))
+    c.run()
+    big = float(torch.tensor(3e38, dtype=c.dt))
+    # probabilities and their sum round (as in the bounds of the oracle: 4 half steps of binary32 a key), a result once
+    assert ((c.out.double() / big - 1).abs() <= 2 * half_step(c.dt) + 4 * (max(c.lengths) + 16) * U32).all()
