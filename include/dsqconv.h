@@ -658,7 +658,9 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
  * tree       device, uint64 [rows][tree_words]: bit b % 64 of word b / 64; keys past the last word are
  *            not seen; or NULL
  * workspace  device, dsq_attention_cache_bytes(..) bytes; of no other call that may run at the same
- *            time, captured graphs included
+ *            time, captured graphs included.  Its size and the launch go by sequences times max_rows: a
+ *            long prompt and single tokens are better two calls (2048 rows over 8192 keys and 63 tokens
+ *            over 4096: 64 MB, 3 MB and 0.61 ms together, 2.1 GB and 1.28 ms in one call)
  * A sequence has at most 2^30 keys (table_pages * page), all sequences together 2^37 by their tables, and
  * max_rows times the heads that share a key head are at most 2^30; rows times q_heads are below 2^26, and
  * sequences times kv_heads, times 128s of rows a key head where there are more than 32, below 2^22

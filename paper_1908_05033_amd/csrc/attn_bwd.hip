@@ -9,8 +9,8 @@
 // in registers (attn_device.h).
 //
 // Seven products of the scores' size, where one kernel with atomics would have five.  Measured, bfloat16, 4 x 2048 rows, causal, 16 heads
-// of 128 in four groups: queries 120 us (45 % of the matrix units' cycles), keys 200 us (34 %; LDS 37 %: one workgroup of eight waves a
-// compute unit goes through its phases in step).  binary32, 80 elements, 3 sequences of up to 701 rows: 48 and 55 us, few workgroups of one wave a SIMD.
+// of 128 in four groups: queries 118 us (44 % of the matrix units' cycles), keys 195 us (34 %; LDS 35 %: one workgroup of eight waves a
+// compute unit goes through its phases in step).  binary32, 80 elements, 3 sequences of up to 701 rows: 48 and 56 us, few workgroups of one wave a SIMD.
 #include <type_traits>
 
 #include "attn_device.h"

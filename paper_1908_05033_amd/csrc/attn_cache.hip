@@ -10,7 +10,9 @@
 // Bound by memory: every key and value is read once a key head (once for each 128 rows of it).  Measured, bfloat16, 128 elements: 32
 // sequences of up to 8192 keys, 503 MB, 104 us and 6 for the join (4.8 TB/s; a large copy reaches 5.07); one of 131072 keys, 268 MB,
 // 53 + 8; one of 500 keys, one launch, 9.1: a chain of dependent loads (length, page, keys, values).  float16, 8 trees of 48 drafted
-// tokens, up to 4096 keys, 53 + 11: two tiles of rows read the same keys, and a chunk is a few tiles long.
+// tokens, up to 4096 keys, 53 + 11: two tiles of rows read the same keys, and a chunk is a few tiles long.  binary32, one sequence of
+// 131072 keys, 1.07 GB, 280 us (3.8 TB/s: one workgroup a compute unit).  256 to 16384 sequences of 256 keys 4.0 to 4.1 TB/s: every
+// workgroup looks at the lengths of all sequences, which does not show.  2048 rows over 8192 keys 374 us.
 #include "attn_cache_plan.h"
 #include "attn_device.h"
 

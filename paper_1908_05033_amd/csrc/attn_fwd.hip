@@ -8,9 +8,9 @@
 // lanes of a row, and the probabilities are the second operand of V^T P^T as they lie in registers (attn_device.h).
 //
 // Bound by the matrix units and the vector instructions of the softmax beside them: two waves a SIMD, one's products under the other's
-// exponentials.  Measured, bfloat16, 128 elements, causal: 16384 rows, 16 heads 1077 us (1021 TFLOP/s; a library product of 8192^3 reaches
-// 1131; 52 % of the matrix units' cycles), 4096 rows, 32 heads 146 us (939).  float16, 64 elements, 16 sequences of up to 1000
-// rows 33 us: the walk over the longest one's keys.
+// exponentials.  Measured, bfloat16, 128 elements, causal: 16384 rows, 16 heads 1025 us (1073 TFLOP/s; a library product of 8192^3 reaches
+// 1131; 53 % of the matrix units' cycles), 4096 rows, 32 heads 139 us (988).  float16, 64 elements, 16 sequences of up to 1000
+// rows 34 us, 20 % of the matrix units' cycles: a walk over 1024 keys takes 18 by itself, and the walks do not go out by their lengths.
 #include <type_traits>
 
 #include "attn_device.h"
