@@ -646,7 +646,8 @@ dsq_status dsq_attention_bwd(const void *q, int64_t q_row, int64_t q_head, const
  * 0 .. m - 1; its rows are the tokens m - n .. m - 1, and each sees all keys before m - n and of the
  * others, drafted key b = 0 .. n - 1, those before it and itself (tree NULL), or those whose bit is
  * set in its mask (its own bit too, if it sees itself).  A row that sees no key is zeros, and what a
- * row does not see has no part in it.
+ * row does not see has no part in it (infinities and NaN cost time as for dsq_attention; those among
+ * the drafted keys for all rows that do not see them).
  *
  * q          device, [rows][q_heads] heads
  * q_starts   device, or NULL: one row a sequence (rows = sequences)
