@@ -597,7 +597,7 @@ dsq_status dsq_qk_norm_rope_bwd(const void *q, int64_t q_row, int64_t q_head,
  * j <= i + m - n (causal != 0: its last row sees all).  A row that sees no key is zeros.  What a row
  * does not see has no part in it, infinities and NaN included.
  * (Infinities and NaN cost time: up to four times the call's where all later rows see them, and the rows
- * before one in its tile, at most 63 a head, are formed one by one: 4 ms each at 16384 keys.  So is a row
+ * before one in its tile, at most 94 a head, are formed one by one: 4 ms each at 16384 keys.  So is a row
  * of values so near the end of binary32 that their sum passes it.)
  *
  * q_starts, k_starts   device; k_starts NULL: as q_starts; both NULL: one sequence of all rows

@@ -448,8 +448,9 @@ __device__ __forceinline__ void attend(const E *kt, const E *vt, int in, const t
 // infinity or NaN early in a sequence is seen by all rows after it, so a row is looked at in three steps:
 //   - the sum of its softmax is not finite: it sees a score that is NaN or plus infinity (hidden keys have no part in the sum), and nothing of it is finite;
 //   - each of its elements that is not finite sees a value that is not: the sum of those, infinity or NaN, is the element;
-//   - else the row is formed again from the keys it sees alone, by one wave: 2 to 4 ms for a row of 16384 keys.  In a causal prompt those are at most 63 rows
-//     a head for each value that is not finite (the ones before it in its tile), and the rows whose sums pass binary32.
+//   - else the row is formed again from the keys it sees alone, by one wave: 2 to 4 ms for a row of 16384 keys.  In a causal prompt those are at most 94 rows
+//     a head for each value that is not finite (the ones before it in its tile of 64 keys and beside those in their 32 rows), and the rows whose sums pass
+//     binary32.
 // Keys: `int count()`, `int64_t place(j)` of key j, negative if it is not seen, `const E *key(place)`, `const E *value(place)`.
 
 // Elements of a head, bit d % 64 of word d / 64: NaN, and infinities.
